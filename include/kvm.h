@@ -8,7 +8,8 @@
  *   kvm_identify_sets  contiguous merging sets + pivot of each set
  *   kvm_merge          Gaussian-kernel weighted merge into a compacted cache
  * (kvm_evict and kvm_evict_merge_values are comparison workloads: plain eviction by the same
- *  scores, and eviction with the evicted values averaged into the kept ones)
+ *  scores, and eviction with the evicted values averaged into the kept ones), and answering from the
+ * compacted cache takes two calls a layer: kvm_paged_append and kvm_prefix_attn.
  *
  * Conventions for every call
  *   - Every tensor pointer is a DEVICE pointer to contiguous memory, innermost
@@ -379,6 +380,97 @@ kvm_status kvm_evict(const kvm_shape *shape, const kvm_params *params, const voi
 kvm_status kvm_evict_merge_values(const kvm_shape *shape, const kvm_params *params, const void *K, const void *V,
                                   const float *mass, int32_t *kept, int32_t *n_kept, void *K_out, void *V_out,
                                   void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Answering from the compacted cache.  The paper stops at the compressed prefill; what follows are the two
+ * calls a program makes for every generated token (or for a further question of many tokens), layer by
+ * layer, on the rows that kvm_merge left and on a paged cache of the tokens that came after the prompt:
+ *
+ *   kvm_paged_append   rotate the new queries and keys to their positions, store keys and values in pages
+ *   kvm_prefix_attn    attention over the compacted prompt, shared by all rows that answer it, and over
+ *                      each row's own pages
+ *
+ * For both, shape means: B rows, T = N new tokens a row (right-padded), of which seq_lens[b] are there
+ * (NULL: all T); H_kv, G, d and dtype as elsewhere.  New tokens are token-major as a projection leaves them:
+ * q (B, T, H_kv*G, d), k and v (B, T, H_kv, d), the heads of a token contiguous, consecutive tokens (also
+ * of consecutive rows) *_stride elements apart, so that views of one fused projection need no copy.
+ * Pointers and strides have to be multiples of 16 bytes.  A call takes up to 2^22 tokens (B * N) and 2^29 head rows
+ * (B * N * H_kv * (G + 2)).
+ */
+typedef struct {
+    void *K, *V;              /* DEVICE (n_pages, H_kv, page_size, d) dtype: one layer's pool of pages     */
+    const int32_t *table;     /* DEVICE (B, max_pages): the page that holds tokens [i*page_size,
+                                 (i+1)*page_size) of a row; entries outside [0, n_pages) mean that the
+                                 row has no such page                                                      */
+    int32_t n_pages;
+    int32_t page_size;        /* a power of two, 1 .. 65536                                                */
+    int32_t max_pages;        /* max_pages * page_size <= 2^22                                             */
+} kvm_pages;
+
+typedef struct {
+    const float *inv_freq;    /* DEVICE [rot_dim / 2]: angle per position in radians; not read if rot_dim == 0 */
+    int32_t rot_dim;          /* leading dimensions of a head that turn: 0 .. d, a multiple of 16          */
+    int32_t interleaved;      /* 0: dimensions i and i + rot_dim/2 are a pair; 1: 2i and 2i + 1            */
+} kvm_rotation;
+
+typedef struct {
+    const void *K, *V;        /* DEVICE (P, H_kv, capacity, d) dtype: K_out, V_out of kvm_merge            */
+    const int32_t *lens;      /* DEVICE (P, H_kv): states of every head, n_sets of kvm_identify_sets (clamped
+                                 to [0, capacity]; rows beyond are never read), or NULL: capacity           */
+    const int32_t *row_start; /* DEVICE [P + 1], ascending: rows [row_start[p], row_start[p+1]) answer prompt
+                                 p, a row outside all of them has no prefix; NULL: B / P rows each          */
+    int32_t P;                /* prompts                                                                    */
+    int32_t capacity;         /* <= 2^22                                                                    */
+} kvm_prefix;
+
+/*
+ * Appends a step's tokens to the paged cache, rotated to their positions on the way.  Token t of row b,
+ * t < seq_lens[b], goes to slot s = past_lens[b] + t of the row and has position x = pos_base[b] + s; with
+ * a = x * inv_freq[i] every pair (u, v) of a query or key head becomes (u cos a - v sin a, v cos a + u sin a);
+ * values, and dimensions from rot_dim on, are stored as they are.  Angles are reduced in 64 bits, pairs turned
+ * in fp32, one rounding to dtype.
+ *   q_new     in   (B, T, H_kv*G, d), or NULL with q_out: keys and values alone
+ *   k_new, v_new  in  (B, T, H_kv, d)
+ *   past_lens in   [B] tokens in the row's pages before the call (clamped to [0, max_pages*page_size])
+ *   pos_base  in   [B] position of a row's slot 0 (its prompt's length), or NULL: 0
+ *   q_out     out  (B, T, H_kv*G, d), contiguous; q_new itself if that is contiguous.  Tokens that are not
+ *                  there (t >= seq_lens[b]) are left as they were
+ *   kv_lens   out  [B] past + new, not beyond max_pages*page_size: what kvm_prefix_attn reads, and past_lens of
+ *                  the next call.  A buffer of its own, not past_lens.
+ * A token whose page the row does not have (see kvm_pages) or whose slot lies behind the table is not stored.
+ * Slots that are written in one call have to be different memory: two rows of a batch may share pages that
+ * they only read.  The call needs no workspace.
+ */
+kvm_status kvm_paged_append(const kvm_shape *shape, const kvm_pages *pages, const kvm_rotation *rotation,
+                            const void *q_new, int64_t q_stride, const void *k_new, int64_t k_stride,
+                            const void *v_new, int64_t v_stride, const int32_t *past_lens,
+                            const int32_t *pos_base, void *q_out, int32_t *kv_lens, void *stream);
+
+/*
+ * Attention of new tokens over their prompt's compacted cache and their row's pages.  Query t of row b, head
+ * h*G + g, sees all states of prefix (p, h), p being the row's prompt, and tokens j <= kv_lens[b] - seq_lens[b] + t
+ * of the row's pages (kv_lens counts the new tokens, which are stored already; it is clamped to
+ * max_pages*page_size):
+ *     w = softmax over all of these of q . k / sqrt(d),    out = sum w v,    lse = ln sum exp(q . k / sqrt(d)).
+ * The rows of a prompt are worked on together: its states are read once for all their query heads that share
+ * them.  A query that sees nothing gets out = 0 and lse = -infinity.  Tokens in pages that a row does not have
+ * are not seen.  What a query does not see has no influence, whatever is stored there.
+ *   prefix    in   or NULL: pages alone
+ *   pages     in   or NULL: prefix alone (kv_lens is not read; attention to an encoder's states has this form)
+ *   Q         in   (B, T, H_kv*G, d), tokens q_stride elements apart (q_out of kvm_paged_append: H_kv*G*d)
+ *   kv_lens   in   [B]
+ *   out       out  (B, T, H_kv*G, d) contiguous; tokens t >= seq_lens[b] are left as they were
+ *   lse_opt   out  (B, T, H_kv*G) float32 or NULL
+ *   ws        kvm_prefix_attn_workspace_bytes(), 256-byte aligned; one call at a time
+ * Scores, sums and outputs are accumulated in fp32; 16-bit types round the weights exp(score - running maximum)
+ * once to dtype before they meet the values.  Deterministic: no atomics, and a call on the same shape repeats its
+ * bits.  The order of the sums follows from the sizes in shape, prefix and pages and from the lengths, so a row in another batch
+ * can differ in its last bits.
+ */
+size_t kvm_prefix_attn_workspace_bytes(const kvm_shape *shape, const kvm_prefix *prefix, const kvm_pages *pages);
+kvm_status kvm_prefix_attn(const kvm_shape *shape, const kvm_prefix *prefix, const kvm_pages *pages, const void *Q,
+                           int64_t q_stride, const int32_t *kv_lens, void *out, float *lse_opt, void *ws,
+                           size_t ws_bytes, void *stream);
 
 /*
  * Per-kernel timing for benchmarks (not part of the method; no citation).  While

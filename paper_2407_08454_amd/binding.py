@@ -25,7 +25,8 @@ KVM_SETS_ADJACENT, KVM_SETS_ANCHOR = 0, 1
 
 EXPORTS = ("kvm_params_for_budget", "kvm_out_capacity", "kvm_workspace_bytes", "kvm_attn_mass",
            "kvm_attn_mass_from_lse", "kvm_attn_mass_append", "kvm_sim_append",
-           "kvm_attn_mass_sim", "kvm_identify_sets", "kvm_merge", "kvm_merge_refresh", "kvm_merge_static", "kvm_evict", "kvm_evict_merge_values", "kvm_profile_enable", "kvm_profile_collect", "kvm_profile_disable",
+           "kvm_attn_mass_sim", "kvm_identify_sets", "kvm_merge", "kvm_merge_refresh", "kvm_merge_static", "kvm_evict", "kvm_evict_merge_values", "kvm_paged_append",
+           "kvm_prefix_attn", "kvm_prefix_attn_workspace_bytes", "kvm_profile_enable", "kvm_profile_collect", "kvm_profile_disable",
            "kvm_last_error", "kvm_version")
 
 _TORCH_DTYPE = {torch.float32: KVM_F32, torch.float16: KVM_F16, torch.bfloat16: KVM_BF16}
@@ -42,6 +43,20 @@ class KvmParams(ctypes.Structure):
                 ("value_scale_by_set_size", ctypes.c_int32), ("enforce_budget", ctypes.c_int32),
                 ("weights", ctypes.c_int32), ("pivot_rule", ctypes.c_int32), ("pivot_seed", ctypes.c_uint64),
                 ("set_rule", ctypes.c_int32), ("sim_given", ctypes.c_int32)]
+
+
+class KvmPages(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("table", ctypes.c_void_p), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
+class KvmRotation(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class KvmPrefix(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("row_start", ctypes.c_void_p),
+                ("P", ctypes.c_int32), ("capacity", ctypes.c_int32)]
 
 
 class KvmKernelTime(ctypes.Structure):
@@ -94,6 +109,13 @@ def load_library() -> ctypes.CDLL:
     lib.kvm_evict.restype = ctypes.c_int
     lib.kvm_evict_merge_values.argtypes = lib.kvm_evict.argtypes
     lib.kvm_evict_merge_values.restype = ctypes.c_int
+    SH, PG, PX, I64 = ctypes.POINTER(KvmShape), ctypes.POINTER(KvmPages), ctypes.POINTER(KvmPrefix), ctypes.c_int64
+    lib.kvm_paged_append.argtypes = [SH, PG, ctypes.POINTER(KvmRotation), P, I64, P, I64, P, I64, P, P, P, P, P]
+    lib.kvm_paged_append.restype = ctypes.c_int
+    lib.kvm_prefix_attn_workspace_bytes.argtypes = [SH, PX, PG]
+    lib.kvm_prefix_attn_workspace_bytes.restype = S
+    lib.kvm_prefix_attn.argtypes = [SH, PX, PG, P, I64, P, P, P, P, S, P]
+    lib.kvm_prefix_attn.restype = ctypes.c_int
     lib.kvm_profile_enable.argtypes = [ctypes.c_int32]
     lib.kvm_profile_enable.restype = ctypes.c_int
     lib.kvm_profile_collect.argtypes = [ctypes.POINTER(KvmKernelTime), ctypes.c_int32]
@@ -347,6 +369,155 @@ def kvm_evict(shape: KvmShape, params: KvmParams, K, V, mass, kept, n_kept, K_ou
 def kvm_evict_merge_values(shape: KvmShape, params: KvmParams, K, V, mass, kept, n_kept, K_out, V_out, ws):
     """Comparison workload: as kvm_evict, the evicted values averaged into the nearest kept token's value."""
     _evict("kvm_evict_merge_values", shape, params, K, V, mass, kept, n_kept, K_out, V_out, ws)
+
+
+def make_pages(K_pages: torch.Tensor, V_pages: torch.Tensor, table: torch.Tensor) -> KvmPages:
+    """A layer's paged cache: pools (n_pages, H_kv, page_size, d) and the rows' page table (B, max_pages) int32."""
+    if K_pages.dim() != 4 or K_pages.shape != V_pages.shape or K_pages.dtype != V_pages.dtype or K_pages.dtype not in _TORCH_DTYPE:
+        raise ValueError("K_pages and V_pages must be (n_pages, H_kv, page_size, d) tensors of one supported dtype")
+    if table.dim() != 2 or table.dtype != torch.int32:
+        raise ValueError("the page table must be an int32 tensor of shape (B, max_pages)")
+    _same_device(K_pages, V_pages, table)
+    n_pages, _, page_size, _ = K_pages.shape
+    pages = KvmPages(K_pages.data_ptr(), V_pages.data_ptr(), table.data_ptr(), n_pages, page_size, table.shape[1])
+    pages._refs = (K_pages, V_pages, table)   # the descriptor holds raw pointers: keep the tensors alive
+    return pages
+
+
+def make_rotation(inv_freq: torch.Tensor | None = None, interleaved: bool = False) -> KvmRotation:
+    """Position rotation: inv_freq (rot_dim / 2) float32, radians per position of every pair; None: no rotation."""
+    if inv_freq is None:
+        rotation = KvmRotation(None, 0, 0)
+    else:
+        if inv_freq.dim() != 1 or inv_freq.dtype != torch.float32:
+            raise ValueError("inv_freq must be a float32 vector")
+        _same_device(inv_freq)
+        rotation = KvmRotation(inv_freq.data_ptr(), 2 * inv_freq.numel(), int(bool(interleaved)))
+    rotation._ref = inv_freq
+    return rotation
+
+
+def make_prefix(K: torch.Tensor, V: torch.Tensor, lens: torch.Tensor | None = None,
+                row_start: torch.Tensor | None = None) -> KvmPrefix:
+    """The prompts' compacted caches, K_out and V_out of kvm_merge (P, H_kv, capacity, d): lens (P, H_kv) int32 states
+    a head (n_sets; None: all of them hold capacity), rows [row_start[p], row_start[p + 1]) of a batch answer prompt p (int32, P + 1
+    entries; None: B / P rows each)."""
+    if K.dim() != 4 or K.shape != V.shape or K.dtype != V.dtype or K.dtype not in _TORCH_DTYPE:
+        raise ValueError("K and V must be (P, H_kv, capacity, d) tensors of one supported dtype")
+    _same_device(K, V, lens, row_start)
+    P, H, cap, _ = K.shape
+    if lens is not None and (lens.dtype != torch.int32 or lens.shape != (P, H)):
+        raise ValueError("lens must be int32 of shape (P, H_kv)")
+    if row_start is not None and (row_start.dtype != torch.int32 or row_start.shape != (P + 1,)):
+        raise ValueError("row_start must be int32 of shape (P + 1,)")
+    prefix = KvmPrefix(K.data_ptr(), V.data_ptr(), _ptr(lens), _ptr(row_start), P, cap)
+    prefix._refs = (K, V, lens, row_start)
+    return prefix
+
+
+def make_token_shape(cache: KvmPages | KvmPrefix, T: int, G: int = 1, new_lens: torch.Tensor | None = None,
+                     B: int | None = None) -> KvmShape:
+    """Shape descriptor of T new tokens a row (new_lens[b] of them there; None: all) for the paged cache of the rows, or, with
+    the number of rows given, for a prefix alone."""
+    K = cache._refs[0]
+    if isinstance(cache, KvmPages):
+        B = cache._refs[2].shape[0] if B is None else B
+        if B != cache._refs[2].shape[0]:
+            raise ValueError("the page table has another number of rows")
+    elif B is None:
+        raise ValueError("the number of rows is needed")
+    if new_lens is not None and (new_lens.dtype != torch.int32 or new_lens.shape != (B,) or new_lens.device != K.device):
+        raise ValueError("new_lens must be an int32 tensor of shape (B,) on the cache's device")
+    shape = KvmShape(B, K.shape[1], int(G), int(T), K.shape[3], _TORCH_DTYPE[K.dtype], _ptr(new_lens))
+    shape._seq_lens_ref = new_lens
+    return shape
+
+
+def _check_cache(shape, cache, current):
+    """A cache descriptor fits the shape and lives on the current device, whose stream the call goes to."""
+    K = cache._refs[0]
+    if K.get_device() != current:
+        raise ValueError("the cache is not on the current device")
+    if K.shape[1] != shape.H_kv or K.shape[3] != shape.d or _TORCH_DTYPE[K.dtype] != shape.dtype:
+        raise ValueError("the cache does not match the shape descriptor")
+    if isinstance(cache, KvmPages) and cache._refs[2].shape[0] != shape.B:
+        raise ValueError("the page table does not match the shape descriptor")
+
+
+def _token_stride(name, t, B, T, heads, d, dtype, current):
+    """Elements between consecutive tokens of a (B, T, heads, d) tensor or view whose heads are contiguous."""
+    if t.shape != (B, T, heads, d) or _TORCH_DTYPE.get(t.dtype) != dtype:
+        raise ValueError(f"{name} has shape {tuple(t.shape)} and dtype {t.dtype}, expected {(B, T, heads, d)} of the cache's dtype")
+    if t.get_device() != current:
+        raise ValueError(f"{name} is not on the current GPU")
+    row, token, head, elem = t.stride()
+    if T == 1:
+        token = row
+    if B == 1 and T == 1:
+        token = heads * d
+    if elem != 1 or (head != d and heads > 1) or (B > 1 and row != T * token):
+        raise ValueError(f"{name}: the heads of a token must be contiguous and the tokens evenly spaced")
+    return token
+
+
+def _lens_vector(name, t, B, current):
+    if t.dtype != torch.int32 or t.shape != (B,) or not t.is_contiguous() or t.get_device() != current:
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape (B,) on the current GPU")
+
+
+def kvm_paged_append(shape: KvmShape, pages: KvmPages, rotation: KvmRotation, q_new, k_new, v_new, past_lens, pos_base, q_out,
+                     kv_lens):
+    """The step's keys (rotated) and values into the rows' pages, rotated queries to q_out, kv_lens <- past_lens + new tokens."""
+    B, H, G, T, d = shape.B, shape.H_kv, shape.G, shape.N, shape.d
+    current = torch.cuda.current_device()
+    _check_cache(shape, pages, current)
+    ks = _token_stride("k_new", k_new, B, T, H, d, shape.dtype, current)
+    vs = _token_stride("v_new", v_new, B, T, H, d, shape.dtype, current)
+    qs = 0
+    if q_new is not None:
+        qs = _token_stride("q_new", q_new, B, T, H * G, d, shape.dtype, current)
+        if q_out is None or not q_out.is_contiguous():
+            raise ValueError("q_out must be contiguous")
+        _token_stride("q_out", q_out, B, T, H * G, d, shape.dtype, current)
+    _lens_vector("past_lens", past_lens, B, current)
+    _lens_vector("kv_lens", kv_lens, B, current)
+    if pos_base is not None:
+        _lens_vector("pos_base", pos_base, B, current)
+    if rotation._ref is not None and rotation._ref.get_device() != current:
+        raise ValueError("inv_freq is not on the current GPU")
+    _check("kvm_paged_append", load_library().kvm_paged_append(
+        ctypes.byref(shape), ctypes.byref(pages), ctypes.byref(rotation), _ptr(q_new), qs, k_new.data_ptr(), ks, v_new.data_ptr(), vs,
+        past_lens.data_ptr(), _ptr(pos_base), _ptr(q_out), kv_lens.data_ptr(), _stream()))
+
+
+def kvm_prefix_attn_workspace_bytes(shape: KvmShape, prefix: KvmPrefix | None, pages: KvmPages | None) -> int:
+    need = load_library().kvm_prefix_attn_workspace_bytes(ctypes.byref(shape), None if prefix is None else ctypes.byref(prefix),
+                                                          None if pages is None else ctypes.byref(pages))
+    if need == 0:
+        raise KvmError("kvm_prefix_attn_workspace_bytes", KVM_ERR_INVALID_ARG, load_library().kvm_last_error().decode())
+    return need
+
+
+def kvm_prefix_attn(shape: KvmShape, prefix: KvmPrefix | None, pages: KvmPages | None, Q, kv_lens, out, lse_opt, ws):
+    """out (B, T, H_kv*G, d) <- attention of Q over the rows' shared prefixes and their own pages; lse_opt (B, T, H_kv*G) float32."""
+    B, H, G, T, d = shape.B, shape.H_kv, shape.G, shape.N, shape.d
+    current = torch.cuda.current_device()
+    for cache in (prefix, pages):
+        if cache is not None:
+            _check_cache(shape, cache, current)
+    qs = _token_stride("Q", Q, B, T, H * G, d, shape.dtype, current)
+    _token_stride("out", out, B, T, H * G, d, shape.dtype, current)
+    if not out.is_contiguous() or not ws.is_contiguous() or ws.get_device() != current:
+        raise ValueError("out and ws must be contiguous, ws on the current GPU")
+    if pages is not None:
+        _lens_vector("kv_lens", kv_lens, B, current)
+    if lse_opt is not None and (lse_opt.dtype != torch.float32 or lse_opt.shape != (B, T, H * G) or not lse_opt.is_contiguous() or
+                                lse_opt.get_device() != current):
+        raise ValueError("lse_opt must be a contiguous float32 tensor of shape (B, T, H_kv*G) on the current GPU")
+    _check("kvm_prefix_attn", load_library().kvm_prefix_attn(
+        ctypes.byref(shape), None if prefix is None else ctypes.byref(prefix), None if pages is None else ctypes.byref(pages),
+        Q.data_ptr(), qs, None if pages is None else kv_lens.data_ptr(), out.data_ptr(), _ptr(lse_opt), ws.data_ptr(),
+        ws.numel() * ws.element_size(), _stream()))
 
 
 def kvm_profile_enable(max_launches: int):

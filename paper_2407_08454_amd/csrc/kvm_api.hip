@@ -145,6 +145,71 @@ static size_t ws_plain(const kvm_shape *sh, int cap)
     return std::max(std::max(ws_attn(sh), ws_identify(sh)), merge_refresh_workspace_bytes(*sh, cap)) + 256;
 }
 
+// ---- the paged cache and the compacted prefixes ------------------------------------------
+static bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+static int elem_bytes(const kvm_shape *sh) { return sh->dtype == KVM_F32 ? 4 : 2; }
+
+// rows of B * T tokens with `heads` heads each, `stride` elements apart
+static kvm_status check_rows(const kvm_shape *sh, const char *fn, const char *name, const void *p, int64_t stride, int64_t heads)
+{
+    if (!p) { set_error("%s: %s must not be NULL", fn, name); return KVM_ERR_INVALID_ARG; }
+    if (!aligned16(p) || stride * elem_bytes(sh) % 16 != 0) {
+        set_error("%s: %s and its stride of %lld elements must be multiples of 16 bytes", fn, name, (long long)stride);
+        return KVM_ERR_INVALID_ARG;
+    }
+    if (stride < heads * HEAD_DIM || stride > (1ll << 31)) {
+        set_error("%s: tokens of %s are %lld elements apart, its heads take %lld", fn, name, (long long)stride, (long long)(heads * HEAD_DIM));
+        return KVM_ERR_INVALID_ARG;
+    }
+    return KVM_OK;
+}
+
+static kvm_status check_pages(const kvm_pages *pg, const char *fn)
+{
+    if (pg->n_pages < 0 || pg->max_pages < 0 || pg->page_size < 1 || pg->page_size > 65536 || (pg->page_size & (pg->page_size - 1)) != 0) {
+        set_error("%s: invalid pages (n_pages=%d, max_pages=%d, page_size=%d, a power of two up to 65536)", fn, pg->n_pages, pg->max_pages,
+                  pg->page_size);
+        return KVM_ERR_INVALID_ARG;
+    }
+    if ((int64_t)pg->max_pages * pg->page_size > (1ll << 22)) {
+        set_error("%s: a row of %d pages of %d tokens is too long", fn, pg->max_pages, pg->page_size);
+        return KVM_ERR_UNSUPPORTED;
+    }
+    if ((pg->n_pages > 0 && (!pg->K || !pg->V)) || (pg->max_pages > 0 && !pg->table) || !aligned16(pg->K) || !aligned16(pg->V)) {
+        set_error("%s: the pages' K, V and table must not be NULL, K and V multiples of 16 bytes", fn);
+        return KVM_ERR_INVALID_ARG;
+    }
+    return KVM_OK;
+}
+
+static kvm_status check_prefix(const kvm_shape *sh, const kvm_prefix *px, const char *fn)
+{
+    if (px->P < 0 || px->capacity < 0 || px->capacity > (1 << 22) || (int64_t)px->P * sh->H_kv > (1 << 24)) {
+        set_error("%s: invalid prefix sizes P=%d capacity=%d", fn, px->P, px->capacity);
+        return KVM_ERR_INVALID_ARG;
+    }
+    if (!px->row_start && px->P > 0 && sh->B % px->P != 0) {
+        set_error("%s: %d rows do not divide among %d prompts: row_start is needed", fn, sh->B, px->P);
+        return KVM_ERR_INVALID_ARG;
+    }
+    if (((int64_t)px->P * px->capacity > 0 && (!px->K || !px->V)) || !aligned16(px->K) || !aligned16(px->V)) {
+        set_error("%s: the prefixes' K and V must not be NULL and multiples of 16 bytes", fn);
+        return KVM_ERR_INVALID_ARG;
+    }
+    return KVM_OK;
+}
+
+// tokens and head rows of a call, for the grids
+static kvm_status check_tokens(const kvm_shape *sh, const char *fn)
+{
+    const int64_t tokens = (int64_t)sh->B * sh->N;
+    if (tokens > (1ll << 22) || tokens * sh->H_kv * (sh->G + 2) > (1ll << 29)) {
+        set_error("%s: %lld tokens with %d query and %d key heads are too many for one call", fn, (long long)tokens, sh->H_kv * sh->G, sh->H_kv);
+        return KVM_ERR_UNSUPPORTED;
+    }
+    return KVM_OK;
+}
+
 }  // namespace kvm
 
 using namespace kvm;
@@ -395,6 +460,84 @@ kvm_status kvm_merge_static(const kvm_shape *shape, const kvm_params *params, co
         return KVM_ERR_INVALID_ARG;
     }
     return launch_merge_static(*shape, *params, cap, K, V, set_start, pivot, n_sets, K_out, V_out, w_opt, (hipStream_t)stream);
+}
+
+kvm_status kvm_paged_append(const kvm_shape *shape, const kvm_pages *pages, const kvm_rotation *rotation, const void *q_new,
+                            int64_t q_stride, const void *k_new, int64_t k_stride, const void *v_new, int64_t v_stride,
+                            const int32_t *past_lens, const int32_t *pos_base, void *q_out, int32_t *kv_lens, void *stream)
+{
+    const char *fn = "kvm_paged_append";
+    kvm_status rc = check_shape(shape, fn);
+    if (rc != KVM_OK) return rc;
+    if (!pages || !rotation) { set_error("%s: pages and rotation must not be NULL", fn); return KVM_ERR_INVALID_ARG; }
+    rc = check_pages(pages, fn);
+    if (rc == KVM_OK) rc = check_tokens(shape, fn);
+    if (rc != KVM_OK) return rc;
+    if (rotation->rot_dim < 0 || rotation->rot_dim > HEAD_DIM || rotation->rot_dim % 16 != 0) {
+        set_error("%s: rot_dim %d is not a multiple of 16 up to %d", fn, rotation->rot_dim, HEAD_DIM);
+        return KVM_ERR_UNSUPPORTED;
+    }
+    if (shape->B == 0) return KVM_OK;
+    if (!past_lens || !kv_lens || past_lens == kv_lens) {
+        set_error("%s: past_lens and kv_lens must be two buffers", fn);
+        return KVM_ERR_INVALID_ARG;
+    }
+    if (shape->N > 0) {
+        if (rotation->rot_dim > 0 && !rotation->inv_freq) { set_error("%s: inv_freq must not be NULL", fn); return KVM_ERR_INVALID_ARG; }
+        if (!q_new != !q_out) { set_error("%s: q_new and q_out go together", fn); return KVM_ERR_INVALID_ARG; }
+        const int64_t HG = (int64_t)shape->H_kv * shape->G;
+        if (q_new) {
+            rc = check_rows(shape, fn, "q_new", q_new, q_stride, HG);
+            if (rc == KVM_OK) rc = check_rows(shape, fn, "q_out", q_out, HG * HEAD_DIM, HG);
+            if (rc != KVM_OK) return rc;
+            if (q_new == q_out && q_stride != HG * HEAD_DIM) {
+                set_error("%s: q_out may be q_new only if that is contiguous", fn);
+                return KVM_ERR_INVALID_ARG;
+            }
+        }
+        rc = check_rows(shape, fn, "k_new", k_new, k_stride, shape->H_kv);
+        if (rc == KVM_OK) rc = check_rows(shape, fn, "v_new", v_new, v_stride, shape->H_kv);
+        if (rc != KVM_OK) return rc;
+    }
+    return launch_paged_append(*shape, *pages, *rotation, q_new, q_stride, k_new, k_stride, v_new, v_stride, past_lens, pos_base, q_out,
+                               kv_lens, (hipStream_t)stream);
+}
+
+static kvm_status check_attn_sources(const kvm_shape *shape, const kvm_prefix *prefix, const kvm_pages *pages, const char *fn)
+{
+    kvm_status rc = check_shape(shape, fn);
+    if (rc != KVM_OK) return rc;
+    if (!prefix && !pages) { set_error("%s: prefix and pages must not both be NULL", fn); return KVM_ERR_INVALID_ARG; }
+    rc = check_tokens(shape, fn);
+    if (rc == KVM_OK && prefix) rc = check_prefix(shape, prefix, fn);
+    if (rc == KVM_OK && pages) rc = check_pages(pages, fn);
+    return rc;
+}
+
+size_t kvm_prefix_attn_workspace_bytes(const kvm_shape *shape, const kvm_prefix *prefix, const kvm_pages *pages)
+{
+    if (check_attn_sources(shape, prefix, pages, "kvm_prefix_attn_workspace_bytes") != KVM_OK) return 0;
+    return prefix_attn_workspace_bytes(*shape, prefix, pages);
+}
+
+kvm_status kvm_prefix_attn(const kvm_shape *shape, const kvm_prefix *prefix, const kvm_pages *pages, const void *Q, int64_t q_stride,
+                           const int32_t *kv_lens, void *out, float *lse_opt, void *ws, size_t ws_bytes, void *stream)
+{
+    const char *fn = "kvm_prefix_attn";
+    kvm_status rc = check_attn_sources(shape, prefix, pages, fn);
+    if (rc != KVM_OK) return rc;
+    if ((long long)shape->B * shape->N == 0) return KVM_OK;
+    const int64_t HG = (int64_t)shape->H_kv * shape->G;
+    rc = check_rows(shape, fn, "Q", Q, q_stride, HG);
+    if (rc == KVM_OK) rc = check_rows(shape, fn, "out", out, HG * HEAD_DIM, HG);
+    if (rc != KVM_OK) return rc;
+    if (pages && !kv_lens) { set_error("%s: kv_lens must not be NULL", fn); return KVM_ERR_INVALID_ARG; }
+    const size_t need = prefix_attn_workspace_bytes(*shape, prefix, pages);
+    if (!ws || ws_bytes < need) {
+        set_error("%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : (size_t)0);
+        return KVM_ERR_WORKSPACE;
+    }
+    return launch_prefix_attn(*shape, prefix, pages, Q, q_stride, kv_lens, out, lse_opt, ws, (hipStream_t)stream);
 }
 
 kvm_status kvm_profile_disable(void)

@@ -278,5 +278,11 @@ size_t attn_single_bytes(const kvm_shape &sh);
 kvm_status launch_attn_single(const kvm_shape &sh, const void *Q, const void *K, float *mass, float *part, float *sim, hipStream_t st);
 int attn_lse_stride(int N);
 int attn_row_tiles(int N);
+kvm_status launch_paged_append(const kvm_shape &sh, const kvm_pages &pages, const kvm_rotation &rot, const void *q, int64_t q_stride,
+                               const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *past_lens,
+                               const int32_t *pos_base, void *q_out, int32_t *kv_lens, hipStream_t st);
+size_t prefix_attn_workspace_bytes(const kvm_shape &sh, const kvm_prefix *prefix, const kvm_pages *pages);
+kvm_status launch_prefix_attn(const kvm_shape &sh, const kvm_prefix *prefix, const kvm_pages *pages, const void *Q, int64_t q_stride,
+                              const int32_t *kv_lens, void *out, float *lse, void *ws, hipStream_t st);
 
 }  // namespace kvm
