@@ -1,0 +1,350 @@
+// Building blocks of attention over shared prefixes and paged tails (prefix_attn.hip): which keys a query sees, key tiles
+// of 32 rows in LDS, and the softmax-weighted sum over them on the matrix cores.
+//
+// A wave works on 32 queries (of one KV head) and takes keys 32 at a time.  Scores are formed transposed, S^T = K Q^T: in the 32x32
+// result a lane holds sixteen keys of ONE query (its column), so maximum and sum of a softmax row stay inside the lane but
+// for one exchange with the lane 32 above or below, and the weights, rounded, are already in the lanes in which the second product,
+// O^T = V^T P^T, wants its right operand: its sixteen accumulators of key order 8 (i / 4) + 4 (l / 32) + i % 4 are two fragments of
+// sixteen keys.  The left operand has to have the same keys in its lanes, one value row per lane: four keys of sixteen
+// value columns at a time come out of LDS transposed (ds_read_b64_tr_b16; fp32: plain reads, its fragments hold one key).
+#pragma once
+
+#include "attn_tile.h"
+
+namespace kvm {
+
+constexpr float PX_NONE = -3.0e38f;      // maximum of no score: finite, so that no inf - inf arises
+constexpr float PX_SLACK = 8.f;          // weights may reach 2^8 before a query's accumulators are put on a new maximum
+
+struct PrefixAttnArgs {
+    const void *q, *Kp, *Vp, *Kt, *Vt;
+    const int32_t *lens, *row_start, *table, *new_lens, *kv_lens;
+    void *out;
+    float *lse;
+    float *part, *stat;                   // split calls: accumulators (query rows, parts, d), maximum and sum (query rows, parts, 2)
+    int64_t q_stride;
+    int B, T, H, G, P, cap, n_pages, page_shift, max_pages;
+    int tiles_p, tiles_t;                 // query tiles of all prompts (an upper bound with row_start), of one row
+    int splits_p, splits_t;               // parts that a prefix and a tail are split into
+    float c;                              // log2(e) / sqrt(d): scores in base 2
+};
+
+// 16 bytes of zeros that stand for the rows behind a tile's last key and for missing pages: a key that nobody sees must not bring
+// what lies in its memory into a product, where even a weight of zero would not take a NaN away.
+static __device__ const u32x4 px_zeros = {0u, 0u, 0u, 0u};
+
+// The prompt of row b, or -1.  (The largest p with row_start[p] <= b, so that empty prompts are passed over.)
+__device__ __forceinline__ int prefix_of(const PrefixAttnArgs &a, int b) {
+    if (a.P == 0) return -1;
+    if (!a.row_start) return b / (a.B / a.P);
+    int lo = -1, hi = a.P;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.row_start[mid] <= b) lo = mid; else hi = mid;
+    }
+    return lo >= 0 && b < a.row_start[lo + 1] ? lo : -1;
+}
+__device__ __forceinline__ int prefix_len(const PrefixAttnArgs &a, int p, int h) {
+    return p < 0 ? 0 : a.lens ? min(max(a.lens[(size_t)p * a.H + h], 0), a.cap) : a.cap;
+}
+__device__ __forceinline__ int tail_len(const PrefixAttnArgs &a, int b) {
+    return a.table ? min(max(a.kv_lens[b], 0), a.max_pages << a.page_shift) : 0;
+}
+// keys of one of `splits` parts of n keys: whole tiles, two at least, so that a part has one to load while it works on another
+__device__ __forceinline__ int part_keys(int n, int splits) { return max(((n + splits - 1) / splits + 31) & ~31, 64); }
+
+// value of the lane 32 above or below
+__device__ __forceinline__ float other_half(float v) {
+    const uint32_t a = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(a, a, false, false);
+    const uint32_t r0 = r[0], r1 = r[1];
+    return __builtin_bit_cast(float, (threadIdx.x & 32) ? r0 : r1);
+}
+
+// ---- key tiles ------------------------------------------------------------------------------------
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// 32 rows of CH 16-byte chunks; chunk ch of row r sits at position ch ^ swz(r).  swz makes the sixteen rows that a score fragment
+// reads at one chunk differ, and also the four rows of four chunks that a transposed read takes (fp32: the eight chunks of rows r and
+// r + 4).
+template <typename T> struct KeyTile {
+    static constexpr int CH = Mma<T>::CHUNKS;
+    static constexpr int SLOTS = 32 * CH;
+    static constexpr int RPL = WAVE / CH;                     // rows per load instruction
+    static constexpr int LOADS = 32 / RPL;
+    static constexpr int ROWB = HEAD_DIM * (int)sizeof(T);
+    static __device__ __forceinline__ int swz(int r) {
+        return sizeof(T) == 2 ? ((r & 3) << 2) | ((r >> 2) & 3) : (r & 3) | ((r & 4) << 1) | ((r & 8) >> 1);
+    }
+};
+
+// Byte offsets inside a tile that depend on the lane only.
+template <typename T> struct TileLane {
+    using KT = KeyTile<T>;
+    static constexpr int VADDR = sizeof(T) == 2 ? 8 : 1;
+    int src_row, src_pos;                                     // row (of RPL) and position that this lane's loads fill
+    int kslot[8];                                             // score fragments: slots (fp32: the first eight of sixteen)
+    int vaddr[VADDR];                                         // value fragments: bytes
+    __device__ __forceinline__ TileLane(int lane) {
+        src_row = lane / KT::CH;
+        src_pos = lane % KT::CH;
+        const int row = lane & 31, hf = lane >> 5;
+#pragma unroll
+        for (int f = 0; f < 8; ++f) kslot[f] = row * KT::CH + ((2 * f + hf) ^ KT::swz(row));
+        if constexpr (sizeof(T) == 2) {
+            const int k = (lane & 15) >> 2, col = (((lane >> 4) & 1) << 1) | ((lane >> 1) & 1);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)                       // i = value block + 4 (row & 8)
+                vaddr[i] = ((4 * hf + k) * KT::CH + ((((i & 3) ^ k) << 2) | (col ^ ((i >> 2) << 1) ^ hf))) * 16 + (lane & 1) * 8;
+        } else {
+            vaddr[0] = 0;
+        }
+    }
+    __device__ __forceinline__ u32x4 kfrag(const u32x4 *tile, int f) const {
+        // (fp32: chunks 16 .. 31 are the same positions sixteen further, as swz has four bits)
+        return tile[kslot[f & 7] + (f >> 3) * 16];
+    }
+    // rows pos(lane) + 16-byte chunk of the source that load i of this lane fetches
+    __device__ __forceinline__ int row_of(int i) const { return i * KT::RPL + src_row; }
+    __device__ __forceinline__ int chunk_bytes(int i) const { return (src_pos ^ KT::swz(row_of(i))) * 16; }
+};
+
+// The rows of a prefix slice from j0 on, j0 + 32 > n: zeros behind the last.
+template <typename T>
+__device__ __forceinline__ void load_prefix_tile(const TileLane<T> &tl, const char *K, const char *V, int j0, int n, u32x4 *kt, u32x4 *vt, int first,
+                                                 int step) {
+    using KT = KeyTile<T>;
+    const char *kb = K + (size_t)j0 * KT::ROWB, *vb = V + (size_t)j0 * KT::ROWB;
+    if (j0 + 32 <= n) {
+#pragma unroll
+        for (int i = 0; i < KT::LOADS; ++i) {
+            if (step > 1 && i % step != first) continue;
+            const uint32_t off = tl.row_of(i) * KT::ROWB + tl.chunk_bytes(i);
+            __builtin_amdgcn_global_load_lds((gptr_t)(kb + off), (lptr_t)(kt + i * WAVE), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((gptr_t)(vb + off), (lptr_t)(vt + i * WAVE), 16, 0, 0);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < KT::LOADS; ++i) {
+            if (step > 1 && i % step != first) continue;
+            const uint32_t off = tl.row_of(i) * KT::ROWB + tl.chunk_bytes(i);
+            const bool there = j0 + tl.row_of(i) < n;
+            const char *ks = there ? kb + off : (const char *)&px_zeros, *vs = there ? vb + off : (const char *)&px_zeros;
+            __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(kt + i * WAVE), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(vt + i * WAVE), 16, 0, 0);
+        }
+    }
+}
+
+// A row's page table, 64 entries at a time, one a lane.
+struct PageWindow {
+    const int32_t *table;
+    int first, entry, pages, n_pages;
+    __device__ __forceinline__ PageWindow(const PrefixAttnArgs &a, int b) : table(a.table + (size_t)b * a.max_pages), first(-1), entry(-1),
+                                                                            pages(a.max_pages), n_pages(a.n_pages) {}
+    // entries of pages [lo, hi], hi - lo < 64 (wave-uniform)
+    __device__ __forceinline__ void need(int lo, int hi) {
+        if (first >= 0 && lo >= first && hi < first + 64) return;
+        first = lo;
+        const int i = lo + (int)(threadIdx.x & 63);
+        entry = i < pages ? table[i] : -1;
+        if (entry >= n_pages) entry = -1;
+    }
+    __device__ __forceinline__ int page(int i) const { return __shfl(entry, i - first, WAVE); }
+};
+
+// Tokens [j0, j0 + 32) of a row's pages below n.  Returns which of them are there, one bit each.
+template <typename T>
+__device__ __forceinline__ uint32_t load_tail_tile(const TileLane<T> &tl, const PrefixAttnArgs &a, PageWindow &win, int h, int j0, int n, u32x4 *kt,
+                                                   u32x4 *vt, int first, int step) {
+    using KT = KeyTile<T>;
+    const int lane = threadIdx.x & 63;
+    const int shift = a.page_shift, mask = (1 << shift) - 1, last = min(j0 + 31, n - 1);
+    win.need(j0 >> shift, last >> shift);
+    const uint32_t below = n - j0 >= 32 ? 0xFFFFFFFFu : (1u << (n - j0)) - 1;
+    // where the row of token j0 + (lane % 32) begins, in rows of the pool
+    const int j = min(j0 + (lane & 31), last);
+    const int page = win.page(j >> shift);
+    const uint32_t there = (uint32_t)__ballot(page >= 0) & below;
+    const int64_t row = (((int64_t)page * a.H + h) << shift) + (j & mask);
+    const uint32_t lo = (uint32_t)row, hi = (uint32_t)(row >> 32);
+#pragma unroll
+    for (int i = 0; i < KT::LOADS; ++i) {
+        if (step > 1 && i % step != first) continue;
+        const int r = tl.row_of(i);
+        const uint64_t at = (((uint64_t)(uint32_t)__shfl((int)hi, r, WAVE) << 32) | (uint32_t)__shfl((int)lo, r, WAVE)) * KT::ROWB + tl.chunk_bytes(i);
+        const bool ok = (there >> r) & 1;
+        const char *ks = ok ? (const char *)a.Kt + at : (const char *)&px_zeros, *vs = ok ? (const char *)a.Vt + at : (const char *)&px_zeros;
+        __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(kt + i * WAVE), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(vt + i * WAVE), 16, 0, 0);
+    }
+    return there;
+}
+
+// ---- 32 queries of a wave -------------------------------------------------------------------------
+
+template <typename T> struct Queries {
+    using M = Mma<T>;
+    u32x4 q[M::FRAGS];
+    f32x16 o[4];                          // O^T: value block, accumulator i = value 32 block + acc_row(i), column = query
+    float m, l;                           // running reference (base 2) and this lane's part of the sum
+    int sees;                             // tail tokens that this lane's query sees
+    bool valid;
+    int64_t row;                          // its row in out
+
+    // query `lin` = (b T + t) G + g of head h, `end`: the first that is not this tile's
+    __device__ __forceinline__ void init(const PrefixAttnArgs &a, int64_t lin, int64_t end, int h) {
+        const int hf = (threadIdx.x >> 5) & 1;
+        const int64_t token = lin / a.G;
+        const int g = (int)(lin - token * a.G), b = (int)(token / a.T), t = (int)(token - (int64_t)b * a.T);
+        valid = lin < end;
+        sees = 0;
+        if (valid) {
+            const int n_new = clamp_len(a.new_lens, b, a.T), n_tail = tail_len(a, b);
+            valid = t < n_new;
+            sees = valid ? min(max(n_tail - n_new + t + 1, 0), n_tail) : 0;
+        }
+        row = token * (a.H * a.G) + h * a.G + g;
+        const char *src = (const char *)((const T *)a.q + token * a.q_stride + (int64_t)(h * a.G + g) * HEAD_DIM);
+#pragma unroll
+        for (int f = 0; f < M::FRAGS; ++f) {
+            u32x4 v = {0u, 0u, 0u, 0u};
+            if (valid) v = *reinterpret_cast<const u32x4 *>(src + (2 * f + hf) * 16);
+            q[f] = v;
+        }
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+        m = PX_NONE;
+        l = 0.f;
+    }
+
+    __device__ __forceinline__ f32x16 scores(const TileLane<T> &tl, const u32x4 *kt) const {
+        f32x16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int f = 0; f < M::FRAGS; ++f) M::mma(s, tl.kfrag(kt, f), q[f]);
+        return s;
+    }
+
+    // keys that are not there, and tokens from `sees` on, out of the scores
+    __device__ __forceinline__ void mask(f32x16 &s, uint32_t there, int left) const {
+        const int hf = (threadIdx.x >> 5) & 1;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = 8 * (i >> 2) + (i & 3) + 4 * hf;
+            if (!((there >> r) & 1) || r >= left) s[i] = -INFINITY;
+        }
+    }
+
+    // the tile's weights, taken against a reference that may lag behind the maximum by PX_SLACK
+    __device__ __forceinline__ void weights(f32x16 &s, float c) {
+        float top = max16(s);
+        top = fmaxf(top, other_half(top)) * c;
+        if (__ballot(top > m + PX_SLACK)) {
+            const float next = fmaxf(m, top), scale = __builtin_amdgcn_exp2f(m - next);
+            l *= scale;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= scale;
+            m = next;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -m));
+        float p0 = 0.f, p1 = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) { p0 += s[i]; p1 += s[i + 1]; }
+        l += p0 + p1;
+    }
+
+    // O^T += V^T P^T.  The weights are rounded to the cache type here (half a step of each weight; fp32 keeps them).
+    __device__ __forceinline__ void values(const TileLane<T> &tl, const f32x16 &w, const u32x4 *vt) {
+        if constexpr (sizeof(T) == 2) {
+            const __attribute__((address_space(3))) char *base = (const __attribute__((address_space(3))) char *)(lptr_t)vt;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = w[8 * s + e];
+                const u32x4 p = Elem<T>::from_float(x).v;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    typedef __attribute__((address_space(3))) s16x4 *tr_t;
+                    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(base + tl.vaddr[d] + (16 * s) * KeyTile<T>::ROWB)));
+                    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(base + tl.vaddr[4 + d] + (16 * s + 8) * KeyTile<T>::ROWB)));
+                    const u32x4 v = {lo[0], lo[1], hi[0], hi[1]};
+                    M::mma(o[d], v, p);
+                }
+            }
+        } else {
+            const int lane = threadIdx.x & 63, hf = lane >> 5;
+            const float *f = reinterpret_cast<const float *>(vt);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = 8 * (i >> 2) + (i & 3) + 4 * hf;
+                const float wi = w[i];
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const float v = f[(r * KeyTile<T>::CH + ((8 * d + ((lane & 31) >> 2)) ^ KeyTile<T>::swz(r))) * 4 + (lane & 3)];
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, wi, o[d], 0, 0, 0);
+                }
+            }
+        }
+    }
+
+    // One key at a time, for the tiles that values() may not touch (see has_nonfinite): the same state, every lane its own query and half of
+    // the dimensions; a query that does not see the key leaves it out altogether.
+    __device__ __forceinline__ void one_key(const PrefixAttnArgs &a, const T *kr, const T *vr, bool seen) {
+        typedef typename Elem<T>::Raw Raw;
+        const int hf = (threadIdx.x >> 5) & 1;
+        float s = 0.f;
+#pragma unroll
+        for (int f = 0; f < M::FRAGS; ++f) {
+            const u32x4 k = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(kr) + (2 * f + hf) * 16);
+            if constexpr (sizeof(T) == 2) s += RowDot<T>::dot(Raw{k}, Raw{q[f]});
+            else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t ki = k[i], qi = q[f][i];
+                    s = fmaf(__builtin_bit_cast(float, ki), __builtin_bit_cast(float, qi), s);
+                }
+            }
+        }
+        s = (s + other_half(s)) * a.c;
+        if (!seen) return;
+        const float next = fmaxf(m, s), scale = __builtin_amdgcn_exp2f(m - next), w = __builtin_amdgcn_exp2f(s - next);
+        l = l * scale + (hf ? 0.f : w);                       // (the halves' sums are added in the end)
+        m = next;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * scale + w * (float)vr[32 * d + 8 * (i >> 2) + 4 * hf + (i & 3)];
+    }
+};
+
+// Does the value tile hold an infinity or a NaN?  Where some queries of a tile see a key that others do not (later tokens of the same
+// step), a weight of zero would not keep it out of the others' sums.
+template <typename T>
+__device__ __forceinline__ bool has_nonfinite(const u32x4 *vt) {
+    constexpr uint32_t E = sizeof(T) == 4 ? 0x7F800000u : Elem<T>::kDtype == KVM_F16 ? 0x7C00u : 0x7F80u;
+    const int lane = threadIdx.x & 63;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < KeyTile<T>::LOADS; ++i) {
+        const u32x4 v = vt[i * WAVE + lane];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t x = v[k];
+            bad |= (x & E) == E;
+            if (sizeof(T) == 2) bad |= ((x >> 16) & E) == E;
+        }
+    }
+    return __ballot(bad) != 0;
+}
+
+}  // namespace kvm

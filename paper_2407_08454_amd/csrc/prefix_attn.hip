@@ -1,132 +1,298 @@
 // Attention of new tokens over the compacted cache of their prompt and over their row's own pages.
 //
-//   prefix_attn_row_kernel  a workgroup per query row: the keys dealt to its sixteen groups of sixteen lanes, each with the
-//                           running maximum and sum of its keys' softmax; joined through LDS at the end.
+//   prefix_attn_split_kernel  32 queries and a part of their keys a wave.  The keys of a prefix are read once for 32 queries of
+//                             all the prompt's rows; a row's own tail for the queries of that row.
+//   prefix_attn_join_kernel   puts the parts of a query on one maximum and adds them up.
 #include <algorithm>
 
-#include "kvm_common.h"
+#include "prefix_attn.h"
 
 namespace kvm {
 
-constexpr int PX_BLOCK = 256;
-constexpr float PX_NONE = -3.0e38f;      // maximum of no score: finite, so that no inf - inf arises
+constexpr int PX_QUERIES = 32;           // of a wave
+constexpr int PX_JOIN_ROWS = 8;          // query rows of a joining workgroup, 32 lanes each
 
-struct PrefixAttnArgs {
-    const void *q, *Kp, *Vp, *Kt, *Vt;
-    const int32_t *lens, *row_start, *table, *new_lens, *kv_lens;
-    void *out;
-    float *lse;
-    int64_t q_stride;
-    int B, T, H, G, P, cap, n_pages, page_shift, max_pages;
-    float c;                              // log2(e) / sqrt(d): scores in base 2
-};
-
-// The prompt of row b, or -1.  (The largest p with row_start[p] <= b, so that empty prompts are passed over.)
-__device__ __forceinline__ int prefix_of(const PrefixAttnArgs &a, int b) {
-    if (a.P == 0) return -1;
-    if (!a.row_start) return b / (a.B / a.P);
-    int lo = -1, hi = a.P;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.row_start[mid] <= b) lo = mid; else hi = mid;
+// Query tile `tile` of `per_tile` queries of all prompts: its prompt and queries [lin, end) in the order (row, token, head of the group).
+struct QueryTile { int p; int64_t lin, end; };
+__device__ __forceinline__ QueryTile find_tile(const PrefixAttnArgs &a, int tile, int per_tile) {
+    const int64_t per_row = (int64_t)a.T * a.G;
+    QueryTile qt = {-1, 0, 0};
+    if (!a.row_start) {
+        const int64_t queries = (a.B / a.P) * per_row;
+        const int tiles = (int)((queries + per_tile - 1) / per_tile);
+        qt.p = tile / tiles;
+        qt.lin = qt.p * queries + (int64_t)(tile - qt.p * tiles) * per_tile;
+        qt.end = (qt.p + 1) * queries;
+        return qt;
     }
-    return lo >= 0 && b < a.row_start[lo + 1] ? lo : -1;
+    const int lane = threadIdx.x & 63;
+    int before = 0;                                          // tiles of the prompts before these 64
+    for (int p0 = 0; p0 < a.P; p0 += WAVE) {
+        const int p = p0 + lane;
+        int first = 0, last = 0;
+        if (p < a.P) {
+            first = min(max(a.row_start[p], 0), a.B);
+            last = min(max(a.row_start[p + 1], first), a.B);
+        }
+        const int tiles = (int)(((last - first) * per_row + per_tile - 1) / per_tile);
+        int sum = tiles;                                     // inclusive scan
+#pragma unroll
+        for (int d = 1; d < WAVE; d *= 2) {
+            const int v = __shfl_up(sum, d, WAVE);
+            if (lane >= d) sum += v;
+        }
+        const uint64_t reached = __ballot(before + sum > tile);
+        if (reached) {
+            const int at = __ffsll((unsigned long long)reached) - 1;
+            qt.p = p0 + at;
+            const int row0 = __shfl(first, at, WAVE), row1 = __shfl(last, at, WAVE);
+            const int start = before + __shfl(sum - tiles, at, WAVE);
+            qt.lin = row0 * per_row + (int64_t)(tile - start) * per_tile;
+            qt.end = row1 * per_row;
+            return qt;
+        }
+        before += __shfl(sum, WAVE - 1, WAVE);
+    }
+    return qt;
 }
-__device__ __forceinline__ int prefix_len(const PrefixAttnArgs &a, int p, int h) {
-    return p < 0 ? 0 : a.lens ? min(max(a.lens[(size_t)p * a.H + h], 0), a.cap) : a.cap;
+
+// What bounds it: the read of the keys and values.  A wave has two stages of 32 keys in LDS, one on its way while it works on the other, so
+// five waves of a compute unit (160 KB of LDS) keep 80 KB in flight; nobody waits for anybody.
+template <typename T>
+__global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_split_kernel(PrefixAttnArgs a)
+{
+    using KT = KeyTile<T>;
+    __shared__ u32x4 k_a[KT::SLOTS], v_a[KT::SLOTS], k_b[KT::SLOTS], v_b[KT::SLOTS];   // (four objects: see attn_lse_kernel)
+    const int lane = threadIdx.x;
+    const int units_p = a.tiles_p * a.H * a.splits_p;
+    int u = blockIdx.x;
+    const bool tail = u >= units_p;
+    int h, s, b = 0, p = -1, j0, end, least = 0;              // least: tokens that every query of the tile sees
+    int64_t lin, lin_end;
+    if (!tail) {
+        // the query tiles of a part read the same keys: on one XCD
+        const int groups = a.H * a.splits_p;
+        int group, tile;
+        if (groups % 8 == 0) {
+            const int slot = u >> 3;
+            group = slot / a.tiles_p * 8 + (u & 7);
+            tile = slot % a.tiles_p;
+        } else {
+            group = u / a.tiles_p;
+            tile = u % a.tiles_p;
+        }
+        h = group % a.H;
+        s = group / a.H;
+        const QueryTile qt = find_tile(a, tile, PX_QUERIES);
+        p = qt.p;
+        if (p < 0) return;
+        lin = qt.lin;
+        lin_end = qt.end;
+        const int n = prefix_len(a, p, h), part = part_keys(n, a.splits_p);
+        j0 = s * part;
+        end = min(n, j0 + part);
+    } else {
+        u -= units_p;
+        s = u % a.splits_t;
+        u /= a.splits_t;
+        const int tile = u % a.tiles_t;
+        u /= a.tiles_t;
+        h = u % a.H;
+        b = u / a.H;
+        const int n_new = clamp_len(a.new_lens, b, a.T), n = tail_len(a, b), part = part_keys(n, a.splits_t);
+        const int64_t row_lin = (int64_t)b * a.T * a.G;
+        lin = row_lin + (int64_t)tile * PX_QUERIES;
+        lin_end = row_lin + (int64_t)n_new * a.G;
+        if (lin >= lin_end) return;
+        const int t_first = (int)((lin - row_lin) / a.G), t_last = (int)((min(lin + PX_QUERIES, lin_end) - 1 - row_lin) / a.G);
+        least = min(max(n - n_new + t_first + 1, 0), n);
+        j0 = s * part;
+        end = min(min(max(n - n_new + t_last + 1, 0), n), j0 + part);
+    }
+    if (j0 >= end) return;
+
+    const TileLane<T> tl(lane);
+    Queries<T> qs;
+    const char *Kp = nullptr, *Vp = nullptr;
+    PageWindow win(a, b);
+    if (!tail) {
+        const size_t at = ((size_t)p * a.H + h) * a.cap * KT::ROWB;
+        Kp = (const char *)a.Kp + at;
+        Vp = (const char *)a.Vp + at;
+    }
+    auto load = [&](int j, u32x4 *kt, u32x4 *vt) -> uint32_t {
+        if (tail) return load_tail_tile<T>(tl, a, win, h, j, end, kt, vt, 0, 1);
+        load_prefix_tile<T>(tl, Kp, Vp, j, end, kt, vt, 0, 1);
+        return end - j >= 32 ? 0xFFFFFFFFu : (1u << (end - j)) - 1;
+    };
+    int stop = end;                                          // tokens from here on one at a time
+    auto work = [&](int j, uint32_t there, const u32x4 *kt, const u32x4 *vt) {
+        f32x16 x = qs.scores(tl, kt);
+        const bool mixed = tail && j + 32 > least;
+        if (mixed || there != 0xFFFFFFFFu) {
+            qs.mask(x, there, tail ? qs.sees - j : 32);
+            if (mixed && a.T > 1 && has_nonfinite<T>(vt)) { stop = j; return; }
+        }
+        qs.weights(x, a.c);
+        qs.values(tl, x, vt);
+    };
+    uint32_t there_a = load(j0, k_a, v_a), there_b = 0;
+    qs.init(a, lin + (lane & 31), lin_end, h);
+    for (int j = j0;;) {
+        if (j + 32 < end) {
+            wait_lds();
+            there_b = load(j + 32, k_b, v_b);
+            wait_vmcnt<2 * KT::LOADS>();
+        } else {
+            wait_vmcnt<0>();
+        }
+        work(j, there_a, k_a, v_a);
+        j += 32;
+        if (j >= end || stop < end) break;
+        if (j + 32 < end) {
+            wait_lds();
+            there_a = load(j + 32, k_a, v_a);
+            wait_vmcnt<2 * KT::LOADS>();
+        } else {
+            wait_vmcnt<0>();
+        }
+        work(j, there_b, k_b, v_b);
+        j += 32;
+        if (j >= end || stop < end) break;
+    }
+    wait_vmcnt<0>();
+    for (int j = stop; j < end; ++j) {                       // (tails only)
+        const int page = a.table[(size_t)b * a.max_pages + (j >> a.page_shift)];
+        if (page < 0 || page >= a.n_pages) continue;
+        const size_t at = ((((size_t)page * a.H + h) << a.page_shift) + (j & ((1 << a.page_shift) - 1))) * HEAD_DIM;
+        qs.one_key(a, (const T *)a.Kt + at, (const T *)a.Vt + at, j < qs.sees);
+    }
+
+    const float l = qs.l + other_half(qs.l);
+    if (!qs.valid) return;
+    const size_t at = (size_t)qs.row * (a.splits_p + a.splits_t) + (tail ? a.splits_p + s : s);
+    float *dst = a.part + at * HEAD_DIM + 4 * (lane >> 5);
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x4 v = {qs.o[d][4 * i], qs.o[d][4 * i + 1], qs.o[d][4 * i + 2], qs.o[d][4 * i + 3]};
+            *reinterpret_cast<f32x4 *>(dst + 32 * d + 8 * i) = v;
+        }
+    if (lane < 32) {
+        a.stat[2 * at] = qs.m;
+        a.stat[2 * at + 1] = l;
+    }
 }
-__device__ __forceinline__ int tail_len(const PrefixAttnArgs &a, int b) {
-    return a.table ? min(max(a.kv_lens[b], 0), a.max_pages << a.page_shift) : 0;
+
+// 32 lanes a query row, four dimensions each.
+template <typename T>
+__global__ __launch_bounds__(PX_JOIN_ROWS * 32) void prefix_attn_join_kernel(PrefixAttnArgs a)
+{
+    const int HG = a.H * a.G, lane = threadIdx.x & 31;
+    const int64_t row = (int64_t)blockIdx.x * PX_JOIN_ROWS + (threadIdx.x >> 5);
+    const int64_t token = row / HG;
+    const int b = (int)(token / a.T), t = (int)(token - (int64_t)b * a.T), h = (int)(row - token * HG) / a.G;
+    if (b >= a.B) return;
+    const int n_new = clamp_len(a.new_lens, b, a.T);
+    if (t >= n_new) return;
+    const int n = prefix_len(a, prefix_of(a, b), h), n_tail = tail_len(a, b), sees = min(max(n_tail - n_new + t + 1, 0), n_tail);
+    const int part_p = part_keys(n, max(a.splits_p, 1)), part_t = part_keys(n_tail, max(a.splits_t, 1));
+    const int used_p = (n + part_p - 1) / part_p, used = used_p + (sees + part_t - 1) / part_t;
+    const size_t first = (size_t)row * (a.splits_p + a.splits_t);
+    const auto slot = [&](int k) { return first + (k < used_p ? k : a.splits_p + k - used_p); };
+    float top = PX_NONE;
+    for (int k = lane; k < used; k += 32) top = fmaxf(top, a.stat[2 * slot(k)]);
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d, 32));
+    float total = 0.f;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k = 0; k < used; ++k) {
+        const size_t at = slot(k);
+        const float scale = __builtin_amdgcn_exp2f(a.stat[2 * at] - top);
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(a.part + at * HEAD_DIM + lane * 4);
+        total += a.stat[2 * at + 1] * scale;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += v[i] * scale;
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    T *dst = (T *)a.out + row * HEAD_DIM + lane * 4;
+    T y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = (T)(sum[i] * inv);
+    __builtin_memcpy(dst, y, sizeof(y));
+    if (a.lse && lane == 0) a.lse[row] = total == 0.f ? -INFINITY : (top + __log2f(total)) * 0.69314718055994531f;
+}
+
+// ---- host side ------------------------------------------------------------------------------------
+
+// Parts of a list of keys that is `most` long at most, `units` of them at a time: enough that every compute unit has five waves, of 64 keys each
+// at least; where there is more to read, four times as many, of 512 each, so that the last ones to end leave little of the chip idle.
+static int parts_for(int64_t units, int64_t most)
+{
+    if (units <= 0 || most <= 0) return 0;
+    const int64_t one_round = std::min<int64_t>(1280 / units, most / 64), rounds = std::min<int64_t>(5120 / units, most / 512);
+    return (int)std::max<int64_t>(1, std::max(one_round, rounds));
+}
+
+static void plan(const kvm_shape &sh, const kvm_prefix *prefix, const kvm_pages *pages, PrefixAttnArgs &a)
+{
+    a.B = sh.B; a.T = sh.N; a.H = sh.H_kv; a.G = sh.G; a.new_lens = sh.seq_lens;
+    const int64_t per_row = (int64_t)a.T * a.G;
+    if (prefix && prefix->P > 0 && prefix->capacity > 0) {
+        a.Kp = prefix->K; a.Vp = prefix->V; a.lens = prefix->lens; a.row_start = prefix->row_start; a.P = prefix->P; a.cap = prefix->capacity;
+        a.tiles_p = (int)(a.row_start ? a.B * per_row / PX_QUERIES + a.P : a.P * (((int64_t)(a.B / a.P) * per_row + PX_QUERIES - 1) / PX_QUERIES));
+        const int64_t real = (a.B * per_row + PX_QUERIES - 1) / PX_QUERIES;
+        a.splits_p = parts_for(real * a.H, a.cap);
+    }
+    if (pages && pages->n_pages > 0 && pages->max_pages > 0) {
+        a.Kt = pages->K; a.Vt = pages->V; a.table = pages->table;
+        a.n_pages = pages->n_pages; a.page_shift = __builtin_ctz((unsigned)pages->page_size); a.max_pages = pages->max_pages;
+        a.tiles_t = (int)((per_row + PX_QUERIES - 1) / PX_QUERIES);
+        a.splits_t = parts_for((int64_t)a.B * a.tiles_t * a.H, (int64_t)a.max_pages << a.page_shift);
+    }
+}
+
+static int64_t query_rows(const PrefixAttnArgs &a) { return (int64_t)a.B * a.T * a.H * a.G; }
+
+size_t prefix_attn_workspace_bytes(const kvm_shape &sh, const kvm_prefix *prefix, const kvm_pages *pages)
+{
+    PrefixAttnArgs a = {};
+    plan(sh, prefix, pages, a);
+    return (size_t)query_rows(a) * (a.splits_p + a.splits_t) * (HEAD_DIM + 2) * sizeof(float) + 256;
 }
 
 template <typename T>
-__global__ __launch_bounds__(PX_BLOCK) void prefix_attn_row_kernel(PrefixAttnArgs a)
+static kvm_status launch_t(const PrefixAttnArgs &a, hipStream_t st)
 {
-    typedef typename Elem<T>::Raw Raw;
-    constexpr int GROUPS = PX_BLOCK / 16;
-    __shared__ float acc_of[GROUPS][HEAD_DIM], m_of[GROUPS], l_of[GROUPS];
-    const int HG = a.H * a.G;
-    for (int64_t row = blockIdx.x; row < (int64_t)a.B * a.T * HG; row += gridDim.x) {      // (b, t, head)
-    const int64_t token = row / HG;
-    const int head = (int)(row - token * HG), h = head / a.G;
-    const int b = (int)(token / a.T), t = (int)(token - (int64_t)b * a.T);
-    const int n_new = clamp_len(a.new_lens, b, a.T);
-    if (t >= n_new) continue;
-    const int p = prefix_of(a, b), n_prefix = prefix_len(a, p, h);
-    const int n_tail = min(max(tail_len(a, b) - n_new + t + 1, 0), tail_len(a, b));
-    const int lane = threadIdx.x & 15, group = threadIdx.x >> 4;
-    const Raw q = Elem<T>::load((const T *)a.q + token * a.q_stride + (int64_t)head * HEAD_DIM, lane);
-
-    float m = PX_NONE, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int j = group; j < n_prefix + n_tail; j += GROUPS) {
-        const T *kr, *vr;
-        if (j < n_prefix) {
-            const size_t at = (((size_t)p * a.H + h) * a.cap + j) * HEAD_DIM;
-            kr = (const T *)a.Kp + at;
-            vr = (const T *)a.Vp + at;
-        } else {
-            const int s = j - n_prefix, page = a.table[(size_t)b * a.max_pages + (s >> a.page_shift)];
-            if (page < 0 || page >= a.n_pages) continue;
-            const size_t at = ((((size_t)page * a.H + h) << a.page_shift) + (s & ((1 << a.page_shift) - 1))) * HEAD_DIM;
-            kr = (const T *)a.Kt + at;
-            vr = (const T *)a.Vt + at;
-        }
-        const float x = row16_sum(RowDot<T>::dot(Elem<T>::load(kr, lane), q)) * a.c;
-        float v[8];
-        Elem<T>::to_float(Elem<T>::load(vr, lane), v);
-        const float top = fmaxf(m, x), scale = __builtin_amdgcn_exp2f(m - top), w = __builtin_amdgcn_exp2f(x - top);
-        l = l * scale + w;
-        m = top;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i] = acc[i] * scale + w * v[i];
+    const int64_t units = (int64_t)a.tiles_p * a.H * a.splits_p + (int64_t)a.B * a.tiles_t * a.H * a.splits_t;
+    if (units > 0) {
+        ProfScope prof("prefix_attn_split_kernel", st);
+        hipLaunchKernelGGL(prefix_attn_split_kernel<T>, dim3((unsigned)units), dim3(WAVE), 0, st, a);
+        const kvm_status rc = check_launch("prefix_attn_split_kernel");
+        if (rc != KVM_OK) return rc;
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc_of[group][lane * 8 + i] = acc[i];
-    if (lane == 0) { m_of[group] = m; l_of[group] = l; }
-    __syncthreads();
-    if (threadIdx.x < 16) {
-    float top = PX_NONE, total = 0.f, sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int g = 0; g < GROUPS; ++g) top = fmaxf(top, m_of[g]);
-    for (int g = 0; g < GROUPS; ++g) {
-        const float scale = __builtin_amdgcn_exp2f(m_of[g] - top);
-        total += l_of[g] * scale;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += acc_of[g][lane * 8 + i] * scale;
-    }
-    const float inv = total == 0.f ? 0.f : 1.f / total;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sum[i] *= inv;
-    Elem<T>::store((T *)a.out + row * HEAD_DIM, lane, Elem<T>::from_float(sum));
-    if (a.lse && lane == 0) a.lse[row] = total == 0.f ? -INFINITY : (top + __log2f(total)) * 0.69314718055994531f;
-    }
-    __syncthreads();
-    }
+    ProfScope prof("prefix_attn_join_kernel", st);
+    hipLaunchKernelGGL(prefix_attn_join_kernel<T>, dim3((unsigned)((query_rows(a) + PX_JOIN_ROWS - 1) / PX_JOIN_ROWS)), dim3(PX_JOIN_ROWS * 32), 0,
+                       st, a);
+    return check_launch("prefix_attn_join_kernel");
 }
-
-size_t prefix_attn_workspace_bytes(const kvm_shape &sh, const kvm_prefix *prefix, const kvm_pages *pages) { return 256; }
 
 kvm_status launch_prefix_attn(const kvm_shape &sh, const kvm_prefix *prefix, const kvm_pages *pages, const void *Q, int64_t q_stride,
                               const int32_t *kv_lens, void *out, float *lse, void *ws, hipStream_t st)
 {
     PrefixAttnArgs a = {};
-    a.q = Q; a.q_stride = q_stride; a.out = out; a.lse = lse;
-    a.B = sh.B; a.T = sh.N; a.H = sh.H_kv; a.G = sh.G; a.new_lens = sh.seq_lens;
-    if (prefix) {
-        a.Kp = prefix->K; a.Vp = prefix->V; a.lens = prefix->lens; a.row_start = prefix->row_start; a.P = prefix->P; a.cap = prefix->capacity;
-    }
-    if (pages) {
-        a.Kt = pages->K; a.Vt = pages->V; a.table = pages->table; a.kv_lens = kv_lens;
-        a.n_pages = pages->n_pages; a.page_shift = __builtin_ctz((unsigned)pages->page_size); a.max_pages = pages->max_pages;
-    }
+    plan(sh, prefix, pages, a);
+    a.q = Q; a.q_stride = q_stride; a.kv_lens = kv_lens; a.out = out; a.lse = lse;
+    a.part = (float *)ws;
+    a.stat = a.part + (size_t)query_rows(a) * (a.splits_p + a.splits_t) * HEAD_DIM;
     a.c = (float)(1.4426950408889634 / sqrt((double)sh.d));
-    const dim3 grid((unsigned)std::min((int64_t)a.B * a.T * a.H * a.G, (int64_t)1 << 23));
-    ProfScope prof("prefix_attn_row_kernel", st);
     switch (sh.dtype) {
-    case KVM_F32: hipLaunchKernelGGL(prefix_attn_row_kernel<float>, grid, dim3(PX_BLOCK), 0, st, a); break;
-    case KVM_F16: hipLaunchKernelGGL(prefix_attn_row_kernel<half_t>, grid, dim3(PX_BLOCK), 0, st, a); break;
-    default: hipLaunchKernelGGL(prefix_attn_row_kernel<bf16_t>, grid, dim3(PX_BLOCK), 0, st, a);
+    case KVM_F32: return launch_t<float>(a, st);
+    case KVM_F16: return launch_t<half_t>(a, st);
+    default: return launch_t<bf16_t>(a, st);
     }
-    return check_launch("prefix_attn_row_kernel");
 }
 
 }  // namespace kvm
