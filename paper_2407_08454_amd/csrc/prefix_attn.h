@@ -16,6 +16,8 @@ namespace kvm {
 constexpr float PX_NONE = -3.0e38f;      // maximum of no score: finite, so that no inf - inf arises
 constexpr float PX_SLACK = 8.f;          // weights may reach 2^8 before a query's accumulators are put on a new maximum
 
+enum { PX_WIDE_NONE = 0, PX_WIDE_ROWS = 1, PX_WIDE_PREFIX = 2 };
+
 struct PrefixAttnArgs {
     const void *q, *Kp, *Vp, *Kt, *Vt;
     const int32_t *lens, *row_start, *table, *new_lens, *kv_lens;
@@ -26,6 +28,7 @@ struct PrefixAttnArgs {
     int B, T, H, G, P, cap, n_pages, page_shift, max_pages;
     int tiles_p, tiles_t;                 // query tiles of all prompts (an upper bound with row_start), of one row
     int splits_p, splits_t;               // parts that a prefix and a tail are split into
+    int wide;                             // which of the keys 128 queries share (PX_WIDE_*)
     float c;                              // log2(e) / sqrt(d): scores in base 2
 };
 
@@ -52,6 +55,12 @@ __device__ __forceinline__ int tail_len(const PrefixAttnArgs &a, int b) {
 }
 // keys of one of `splits` parts of n keys: whole tiles, two at least, so that a part has one to load while it works on another
 __device__ __forceinline__ int part_keys(int n, int splits) { return max(((n + splits - 1) / splits + 31) & ~31, 64); }
+
+// the same for the wide kernel, in tiles of 64 keys: those of the prefix, then those of the tail
+__device__ __forceinline__ int wide_part(int n, int n_tail, int splits) {
+    const int tiles = ((n + 63) >> 6) + ((n_tail + 63) >> 6);
+    return max((tiles + splits - 1) / splits, 2);
+}
 
 // value of the lane 32 above or below
 __device__ __forceinline__ float other_half(float v) {
@@ -231,13 +240,16 @@ template <typename T> struct Queries {
         return s;
     }
 
-    // keys that are not there, and tokens from `sees` on, out of the scores
+    // Keys that are not there, and the `left`-th and later ones, out of the scores.  (Bit by bit on the vector ALU: as conditions, sixteen
+    // compares and selects, they took more scalar registers than there are.)
     __device__ __forceinline__ void mask(f32x16 &s, uint32_t there, int left) const {
-        const int hf = (threadIdx.x >> 5) & 1;
+        uint32_t seen = left >= 32 ? there : left <= 0 ? 0u : there & ((1u << left) - 1);
+        seen >>= (threadIdx.x & 32) >> 3;                     // lanes from 32 on: keys four further
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const int r = 8 * (i >> 2) + (i & 3) + 4 * hf;
-            if (!((there >> r) & 1) || r >= left) s[i] = -INFINITY;
+            const float si = s[i];
+            const uint32_t keep = (uint32_t)((int32_t)(seen << (31 - 8 * (i >> 2) - (i & 3))) >> 31);
+            s[i] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, si) & keep) | (0xFF800000u & ~keep));
         }
     }
 
@@ -259,6 +271,27 @@ template <typename T> struct Queries {
         float p0 = 0.f, p1 = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; i += 2) { p0 += s[i]; p1 += s[i + 1]; }
+        l += p0 + p1;
+    }
+
+    // the same for two tiles at once
+    __device__ __forceinline__ void weights(f32x16 &s0, f32x16 &s1, float c) {
+        float top = fmaxf(max16(s0), max16(s1));
+        top = fmaxf(top, other_half(top)) * c;
+        if (__ballot(top > m + PX_SLACK)) {
+            const float next = fmaxf(m, top), scale = __builtin_amdgcn_exp2f(m - next);
+            l *= scale;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= scale;
+            m = next;
+        }
+        float p0 = 0.f, p1 = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { s0[i] = __builtin_amdgcn_exp2f(fmaf(s0[i], c, -m)); p0 += s0[i]; }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { s1[i] = __builtin_amdgcn_exp2f(fmaf(s1[i], c, -m)); p1 += s1[i]; }
         l += p0 + p1;
     }
 
@@ -321,9 +354,16 @@ template <typename T> struct Queries {
         l = l * scale + (hf ? 0.f : w);                       // (the halves' sums are added in the end)
         m = next;
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+        for (int d = 0; d < 4; ++d) {
+            asm volatile("" ::: "memory");                    // (not all the loads at once: they would take the tile loop's registers)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * scale + w * (float)vr[32 * d + 8 * (i >> 2) + 4 * hf + (i & 3)];
+            for (int i = 0; i < 4; ++i) {
+                T v[4];
+                __builtin_memcpy(v, vr + 32 * d + 8 * i + 4 * hf, sizeof(v));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[d][4 * i + e] = o[d][4 * i + e] * scale + w * (float)v[e];
+            }
+        }
     }
 };
 

@@ -56,6 +56,24 @@ __device__ __forceinline__ QueryTile find_tile(const PrefixAttnArgs &a, int tile
     return qt;
 }
 
+// A query's accumulators, maximum and sum into the workspace.
+template <typename T>
+__device__ __forceinline__ void store_part(const PrefixAttnArgs &a, const Queries<T> &qs, size_t at, float l) {
+    const int lane = threadIdx.x & 63;
+    float *dst = a.part + at * HEAD_DIM + 4 * (lane >> 5);
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x4 v = {qs.o[d][4 * i], qs.o[d][4 * i + 1], qs.o[d][4 * i + 2], qs.o[d][4 * i + 3]};
+            *reinterpret_cast<f32x4 *>(dst + 32 * d + 8 * i) = v;
+        }
+    if (lane < 32) {
+        a.stat[2 * at] = qs.m;
+        a.stat[2 * at + 1] = l;
+    }
+}
+
 // What bounds it: the read of the keys and values.  A wave has two stages of 32 keys in LDS, one on its way while it works on the other, so
 // five waves of a compute unit (160 KB of LDS) keep 80 KB in flight; nobody waits for anybody.
 template <typename T>
@@ -64,7 +82,7 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
     using KT = KeyTile<T>;
     __shared__ u32x4 k_a[KT::SLOTS], v_a[KT::SLOTS], k_b[KT::SLOTS], v_b[KT::SLOTS];   // (four objects: see attn_lse_kernel)
     const int lane = threadIdx.x;
-    const int units_p = a.tiles_p * a.H * a.splits_p;
+    const int units_p = a.wide ? 0 : a.tiles_p * a.H * a.splits_p;
     int u = blockIdx.x;
     const bool tail = u >= units_p;
     int h, s, b = 0, p = -1, j0, end, least = 0;              // least: tokens that every query of the tile sees
@@ -170,19 +188,197 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
 
     const float l = qs.l + other_half(qs.l);
     if (!qs.valid) return;
-    const size_t at = (size_t)qs.row * (a.splits_p + a.splits_t) + (tail ? a.splits_p + s : s);
-    float *dst = a.part + at * HEAD_DIM + 4 * (lane >> 5);
+    store_part(a, qs, (size_t)qs.row * (a.splits_p + a.splits_t) + (tail ? a.splits_p + s : s), l);
+}
+
+// The same for many queries: a workgroup of four waves has 128 of them and takes 64 keys at a time, which its waves load together and share.
+// What bounds it: the matrix cores, with the exponentials beside them, and the fragments' way out of LDS (a fragment serves 32 queries).
+// Two workgroups on a compute unit work on their exponentials in turn.
+//   ROWS: the queries of one row and all their keys, prefix and tail one after the other in tiles of 64, in one part or several;
+//   else: the queries of a prompt's rows and a part of their prefix.
+constexpr int PX_WIDE = 128;
+
+// A wave's share of a tile of 64 keys: rows r[0], r[1] of each half.
+template <typename T> struct WideLoad {
+    using KT = KeyTile<T>;
+    static constexpr int N = KT::LOADS / 4;                   // load instructions of a wave per 32 rows of keys
+    uint32_t off[N];
+    int row[N], slot;
+    __device__ __forceinline__ WideLoad(int wave, int lane) : slot(wave * N) {
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x4 v = {qs.o[d][4 * i], qs.o[d][4 * i + 1], qs.o[d][4 * i + 2], qs.o[d][4 * i + 3]};
-            *reinterpret_cast<f32x4 *>(dst + 32 * d + 8 * i) = v;
+        for (int i = 0; i < N; ++i) {
+            row[i] = (wave * N + i) * KT::RPL + lane / KT::CH;
+            off[i] = ((lane % KT::CH) ^ KT::swz(row[i])) * 16;
         }
-    if (lane < 32) {
-        a.stat[2 * at] = qs.m;
-        a.stat[2 * at + 1] = l;
     }
+    // returns which keys are there
+    __device__ __forceinline__ uint64_t prefix(const char *K, const char *V, int j0, int n, u32x4 *kt, u32x4 *vt) const {
+        const char *kb = K + (size_t)j0 * KT::ROWB, *vb = V + (size_t)j0 * KT::ROWB;
+        if (j0 + 64 <= n) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const uint32_t at = (32 * s + row[i]) * KT::ROWB + off[i];
+                    __builtin_amdgcn_global_load_lds((gptr_t)(kb + at), (lptr_t)(kt + s * KT::SLOTS + (slot + i) * WAVE), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((gptr_t)(vb + at), (lptr_t)(vt + s * KT::SLOTS + (slot + i) * WAVE), 16, 0, 0);
+                }
+            return ~0ull;
+        }
+        const uint64_t there = (1ull << (n - j0)) - 1;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uint32_t at = (32 * s + row[i]) * KT::ROWB + off[i];
+                const bool ok = j0 + 32 * s + row[i] < n;
+                const char *ks = ok ? kb + at : (const char *)&px_zeros, *vs = ok ? vb + at : (const char *)&px_zeros;
+                __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(kt + s * KT::SLOTS + (slot + i) * WAVE), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(vt + s * KT::SLOTS + (slot + i) * WAVE), 16, 0, 0);
+            }
+        return there;
+    }
+    __device__ __forceinline__ uint64_t tail(const PrefixAttnArgs &a, PageWindow &win, int h, int j0, int n, u32x4 *kt, u32x4 *vt) const {
+        const int lane = threadIdx.x & 63, shift = a.page_shift, last = min(j0 + 63, n - 1);
+        win.need(j0 >> shift, last >> shift);
+        const int j = min(j0 + lane, last), page = win.page(j >> shift);
+        uint64_t there = __ballot(page >= 0);
+        if (n - j0 < 64) there &= (1ull << (n - j0)) - 1;
+        const int64_t at_row = (((int64_t)page * a.H + h) << shift) + (j & ((1 << shift) - 1));
+        const uint32_t lo = (uint32_t)at_row, hi = (uint32_t)(at_row >> 32);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int r = 32 * s + row[i];
+                const uint64_t at = (((uint64_t)(uint32_t)__shfl((int)hi, r, WAVE) << 32) | (uint32_t)__shfl((int)lo, r, WAVE)) * KT::ROWB + off[i];
+                const bool ok = (there >> r) & 1;
+                const char *ks = ok ? (const char *)a.Kt + at : (const char *)&px_zeros, *vs = ok ? (const char *)a.Vt + at : (const char *)&px_zeros;
+                __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(kt + s * KT::SLOTS + (slot + i) * WAVE), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(vt + s * KT::SLOTS + (slot + i) * WAVE), 16, 0, 0);
+            }
+        return there;
+    }
+};
+
+template <typename T, bool ROWS>
+__global__ __launch_bounds__(4 * WAVE, 2) void prefix_attn_wide_kernel(PrefixAttnArgs a)
+{
+    using KT = KeyTile<T>;
+    __shared__ u32x4 k_a[2 * KT::SLOTS], v_a[2 * KT::SLOTS], k_b[2 * KT::SLOTS], v_b[2 * KT::SLOTS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int tiles = ROWS ? a.B * a.tiles_t : a.tiles_p, splits = a.splits_p;
+    const int groups = a.H * splits;
+    int group, tile;
+    if (groups % 8 == 0) {
+        const int slot = blockIdx.x >> 3;
+        group = slot / tiles * 8 + (blockIdx.x & 7);
+        tile = slot % tiles;
+    } else {
+        group = blockIdx.x / tiles;
+        tile = blockIdx.x % tiles;
+    }
+    const int h = group % a.H, part = group / a.H;
+    int b = 0, p, n_tail = 0, n_new = 0;
+    int64_t lin, lin_end, row_lin = 0;
+    if (ROWS) {
+        b = tile / a.tiles_t;
+        tile = a.tiles_t - 1 - (tile - b * a.tiles_t);        // the last queries see most
+        n_new = clamp_len(a.new_lens, b, a.T);
+        n_tail = tail_len(a, b);
+        row_lin = (int64_t)b * a.T * a.G;
+        lin = row_lin + (int64_t)tile * PX_WIDE;
+        lin_end = row_lin + (int64_t)n_new * a.G;
+        if (lin >= lin_end) return;
+        p = prefix_of(a, b);
+    } else {
+        const QueryTile qt = find_tile(a, tile, PX_WIDE);
+        p = qt.p;
+        if (p < 0) return;
+        lin = qt.lin;
+        lin_end = qt.end;
+    }
+    const int n = prefix_len(a, p, h), tiles_n = (n + 63) >> 6;
+    // tail tokens that the first and the last query of these `count` see
+    const auto sees = [&](int64_t q) { return min(max(n_tail - n_new + (int)((q - row_lin) / a.G) + 1, 0), n_tail); };
+    const int most = ROWS ? sees(min(lin + PX_WIDE, lin_end) - 1) : 0;
+    const int64_t first_q = lin + 32 * wave;
+    const bool idle = first_q >= lin_end;
+    const int wave_least = ROWS && !idle ? sees(first_q) : 0, wave_most = ROWS && !idle ? sees(min(first_q + 32, lin_end) - 1) : 0;
+    const int per_part = wide_part(n, n_tail, splits);
+    int v = part * per_part;
+    const int v_end = min(v + per_part, tiles_n + ((most + 63) >> 6));
+    Queries<T> qs;
+    qs.init(a, first_q + (lane & 31), lin_end, h);
+    int stop = n_tail;                                       // tail tokens from here on one at a time
+    const int tail_end = min(wave_most, (v_end - tiles_n) * 64);
+    if (v < v_end) {
+        const TileLane<T> tl(lane);
+        const WideLoad<T> wl(wave, lane);
+        PageWindow win(a, b);
+        const size_t at = ((size_t)max(p, 0) * a.H + h) * a.cap * KT::ROWB;
+        const char *Kp = (const char *)a.Kp + at, *Vp = (const char *)a.Vp + at;
+        auto load = [&](int v, u32x4 *kt, u32x4 *vt) -> uint64_t {
+            if (!ROWS || v < tiles_n) return wl.prefix(Kp, Vp, 64 * v, n, kt, vt);
+            return wl.tail(a, win, h, 64 * (v - tiles_n), most, kt, vt);
+        };
+        auto work = [&](int v, uint64_t there, const u32x4 *kt, const u32x4 *vt) {
+            const bool tail = ROWS && v >= tiles_n;
+            const int j = 64 * (v - tiles_n);
+            if (idle || (tail && (j >= wave_most || stop < n_tail))) return;
+            f32x16 x0 = qs.scores(tl, kt), x1 = qs.scores(tl, kt + KT::SLOTS);
+            const bool mixed = tail && j + 64 > wave_least;
+            if (mixed || there != ~0ull) {
+                qs.mask(x0, (uint32_t)there, tail ? qs.sees - j : 64);
+                qs.mask(x1, (uint32_t)(there >> 32), tail ? qs.sees - j - 32 : 64);
+                if (mixed && a.T > 1 && (has_nonfinite<T>(vt) || has_nonfinite<T>(vt + KT::SLOTS))) { stop = j; return; }
+            }
+            qs.weights(x0, x1, a.c);
+            qs.values(tl, x0, vt);
+            qs.values(tl, x1, vt + KT::SLOTS);
+        };
+        uint64_t there_a = load(v, k_a, v_a), there_b = 0;
+        for (;;) {
+            wait_vmcnt<0>();
+            wait_lds();
+            barrier_no_fence();
+            if (v + 1 < v_end) there_b = load(v + 1, k_b, v_b);
+            work(v, there_a, k_a, v_a);
+            if (++v >= v_end) break;
+            wait_vmcnt<0>();
+            wait_lds();
+            barrier_no_fence();
+            if (v + 1 < v_end) there_a = load(v + 1, k_a, v_a);
+            work(v, there_b, k_b, v_b);
+            if (++v >= v_end) break;
+        }
+    }
+    if (ROWS && !idle) {
+        for (int j = stop; j < tail_end; ++j) {
+            const int page = a.table[(size_t)b * a.max_pages + (j >> a.page_shift)];
+            if (page < 0 || page >= a.n_pages) continue;
+            const size_t at = ((((size_t)page * a.H + h) << a.page_shift) + (j & ((1 << a.page_shift) - 1))) * HEAD_DIM;
+            qs.one_key(a, (const T *)a.Kt + at, (const T *)a.Vt + at, j < qs.sees);
+        }
+    }
+    const float l = qs.l + other_half(qs.l);
+    if (!qs.valid) return;
+    if (ROWS && splits == 1) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        T *dst = (T *)a.out + qs.row * HEAD_DIM + 4 * (lane >> 5);
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                T y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = (T)(qs.o[d][4 * i + e] * inv);
+                __builtin_memcpy(dst + 32 * d + 8 * i, y, sizeof(y));
+            }
+        if (a.lse && lane < 32) a.lse[qs.row] = l == 0.f ? -INFINITY : (qs.m + __log2f(l)) * 0.69314718055994531f;
+        return;
+    }
+    store_part(a, qs, (size_t)qs.row * (splits + a.splits_t) + part, l);
 }
 
 // 32 lanes a query row, four dimensions each.
@@ -197,8 +393,21 @@ __global__ __launch_bounds__(PX_JOIN_ROWS * 32) void prefix_attn_join_kernel(Pre
     const int n_new = clamp_len(a.new_lens, b, a.T);
     if (t >= n_new) return;
     const int n = prefix_len(a, prefix_of(a, b), h), n_tail = tail_len(a, b), sees = min(max(n_tail - n_new + t + 1, 0), n_tail);
-    const int part_p = part_keys(n, max(a.splits_p, 1)), part_t = part_keys(n_tail, max(a.splits_t, 1));
-    const int used_p = (n + part_p - 1) / part_p, used = used_p + (sees + part_t - 1) / part_t;
+    int used_p, used;
+    if (a.wide == PX_WIDE_ROWS) {
+        const int part = wide_part(n, n_tail, a.splits_p);
+        used_p = used = (((n + 63) >> 6) + ((sees + 63) >> 6) + part - 1) / part;
+    } else {
+        if (a.wide == PX_WIDE_PREFIX) {
+            const int part = wide_part(n, 0, a.splits_p);
+            used_p = (((n + 63) >> 6) + part - 1) / part;
+        } else {
+            const int part = part_keys(n, max(a.splits_p, 1));
+            used_p = (n + part - 1) / part;
+        }
+        const int part_t = part_keys(n_tail, max(a.splits_t, 1));
+        used = used_p + (sees + part_t - 1) / part_t;
+    }
     const size_t first = (size_t)row * (a.splits_p + a.splits_t);
     const auto slot = [&](int k) { return first + (k < used_p ? k : a.splits_p + k - used_p); };
     float top = PX_NONE;
@@ -236,41 +445,78 @@ static int parts_for(int64_t units, int64_t most)
     return (int)std::max<int64_t>(1, std::max(one_round, rounds));
 }
 
+static int tiles_of_prompts(const PrefixAttnArgs &a, int queries)
+{
+    const int64_t per_row = (int64_t)a.T * a.G;
+    return (int)(a.row_start ? a.B * per_row / queries + a.P : a.P * (((int64_t)(a.B / a.P) * per_row + queries - 1) / queries));
+}
+
 static void plan(const kvm_shape &sh, const kvm_prefix *prefix, const kvm_pages *pages, PrefixAttnArgs &a)
 {
     a.B = sh.B; a.T = sh.N; a.H = sh.H_kv; a.G = sh.G; a.new_lens = sh.seq_lens;
     const int64_t per_row = (int64_t)a.T * a.G;
     if (prefix && prefix->P > 0 && prefix->capacity > 0) {
         a.Kp = prefix->K; a.Vp = prefix->V; a.lens = prefix->lens; a.row_start = prefix->row_start; a.P = prefix->P; a.cap = prefix->capacity;
-        a.tiles_p = (int)(a.row_start ? a.B * per_row / PX_QUERIES + a.P : a.P * (((int64_t)(a.B / a.P) * per_row + PX_QUERIES - 1) / PX_QUERIES));
-        const int64_t real = (a.B * per_row + PX_QUERIES - 1) / PX_QUERIES;
-        a.splits_p = parts_for(real * a.H, a.cap);
     }
     if (pages && pages->n_pages > 0 && pages->max_pages > 0) {
         a.Kt = pages->K; a.Vt = pages->V; a.table = pages->table;
         a.n_pages = pages->n_pages; a.page_shift = __builtin_ctz((unsigned)pages->page_size); a.max_pages = pages->max_pages;
+    }
+    const int64_t tail_most = (int64_t)a.max_pages << a.page_shift;
+    if (sh.dtype != KVM_F32) {
+        const int64_t wide_rows = (int64_t)a.B * ((per_row + PX_WIDE - 1) / PX_WIDE) * a.H;
+        const int64_t wide_prompts = a.P ? (a.B * per_row + PX_WIDE - 1) / PX_WIDE * a.H : 0;
+        if (per_row >= PX_WIDE) {
+            a.wide = PX_WIDE_ROWS;
+            a.tiles_t = (int)((per_row + PX_WIDE - 1) / PX_WIDE);
+            a.splits_p = (int)std::max<int64_t>(1, std::min<int64_t>(512 / wide_rows, (a.cap + tail_most) / 256));
+            return;
+        }
+        if (a.P && (a.B / a.P) * per_row >= PX_WIDE) {
+            a.wide = PX_WIDE_PREFIX;
+            a.tiles_p = tiles_of_prompts(a, PX_WIDE);
+            a.splits_p = (int)std::max<int64_t>(1, std::min<int64_t>(512 / wide_prompts, a.cap / 256));
+        }
+    }
+    if (a.P && !a.wide) {
+        a.tiles_p = tiles_of_prompts(a, PX_QUERIES);
+        a.splits_p = parts_for((a.B * per_row + PX_QUERIES - 1) / PX_QUERIES * a.H, a.cap);
+    }
+    if (a.table) {
         a.tiles_t = (int)((per_row + PX_QUERIES - 1) / PX_QUERIES);
-        a.splits_t = parts_for((int64_t)a.B * a.tiles_t * a.H, (int64_t)a.max_pages << a.page_shift);
+        a.splits_t = parts_for((int64_t)a.B * a.tiles_t * a.H, tail_most);
     }
 }
 
 static int64_t query_rows(const PrefixAttnArgs &a) { return (int64_t)a.B * a.T * a.H * a.G; }
+static bool direct(const PrefixAttnArgs &a) { return a.wide == PX_WIDE_ROWS && a.splits_p == 1; }
 
 size_t prefix_attn_workspace_bytes(const kvm_shape &sh, const kvm_prefix *prefix, const kvm_pages *pages)
 {
     PrefixAttnArgs a = {};
     plan(sh, prefix, pages, a);
-    return (size_t)query_rows(a) * (a.splits_p + a.splits_t) * (HEAD_DIM + 2) * sizeof(float) + 256;
+    return (direct(a) ? 0 : (size_t)query_rows(a) * (a.splits_p + a.splits_t) * (HEAD_DIM + 2) * sizeof(float)) + 256;
 }
 
 template <typename T>
 static kvm_status launch_t(const PrefixAttnArgs &a, hipStream_t st)
 {
-    const int64_t units = (int64_t)a.tiles_p * a.H * a.splits_p + (int64_t)a.B * a.tiles_t * a.H * a.splits_t;
+    kvm_status rc = KVM_OK;
+    if constexpr (sizeof(T) == 2) {
+        if (a.wide) {
+            const int64_t blocks = (int64_t)(a.wide == PX_WIDE_ROWS ? a.B * a.tiles_t : a.tiles_p) * a.H * a.splits_p;
+            ProfScope prof("prefix_attn_wide_kernel", st);
+            if (a.wide == PX_WIDE_ROWS) hipLaunchKernelGGL((prefix_attn_wide_kernel<T, true>), dim3((unsigned)blocks), dim3(4 * WAVE), 0, st, a);
+            else hipLaunchKernelGGL((prefix_attn_wide_kernel<T, false>), dim3((unsigned)blocks), dim3(4 * WAVE), 0, st, a);
+            rc = check_launch("prefix_attn_wide_kernel");
+            if (rc != KVM_OK || direct(a)) return rc;
+        }
+    }
+    const int64_t units = a.wide == PX_WIDE_ROWS ? 0 : (a.wide ? 0 : (int64_t)a.tiles_p * a.H * a.splits_p) + (int64_t)a.B * a.tiles_t * a.H * a.splits_t;
     if (units > 0) {
         ProfScope prof("prefix_attn_split_kernel", st);
         hipLaunchKernelGGL(prefix_attn_split_kernel<T>, dim3((unsigned)units), dim3(WAVE), 0, st, a);
-        const kvm_status rc = check_launch("prefix_attn_split_kernel");
+        rc = check_launch("prefix_attn_split_kernel");
         if (rc != KVM_OK) return rc;
     }
     ProfScope prof("prefix_attn_join_kernel", st);
