@@ -16,6 +16,7 @@ namespace kvm {
 constexpr float PX_NONE = -3.0e38f;      // maximum of no score: finite, so that no inf - inf arises
 constexpr float PX_SLACK = 8.f;          // weights may reach 2^8 before a query's accumulators are put on a new maximum
 
+enum { PX_STREAM_NONE = 0, PX_STREAM_TAILS = 1, PX_STREAM_JOIN = 2, PX_STREAM_ALL = 3 };
 enum { PX_WIDE_NONE = 0, PX_WIDE_ROWS = 1, PX_WIDE_PREFIX = 2 };
 
 struct PrefixAttnArgs {
@@ -28,24 +29,27 @@ struct PrefixAttnArgs {
     int B, T, H, G, P, cap, n_pages, page_shift, max_pages;
     int tiles_p, tiles_t;                 // query tiles of all prompts (an upper bound with row_start), of one row
     int splits_p, splits_t;               // parts that a prefix and a tail are split into
-    int wide;                             // which of the keys 128 queries share (PX_WIDE_*)
+    int wide;                             // which of the keys go to 128 queries at a time (PX_WIDE_*)
+    int stream;                           // which of the keys go to the few queries of a row (PX_STREAM_*)
     float c;                              // log2(e) / sqrt(d): scores in base 2
 };
 
-// 16 bytes of zeros that stand for the rows behind a tile's last key and for missing pages: a key that nobody sees must not bring
+// Four rows of zeros that stand for the rows behind a tile's last key and for missing pages: a key that nobody sees must not bring
 // what lies in its memory into a product, where even a weight of zero would not take a NaN away.
-static __device__ const u32x4 px_zeros = {0u, 0u, 0u, 0u};
+static __device__ const u32x4 px_zero_row[4 * HEAD_DIM * sizeof(float) / 16] = {};
 
-// The prompt of row b, or -1.  (The largest p with row_start[p] <= b, so that empty prompts are passed over.)
+// The prompt of row b, or -1, b the same for 32 lanes: the last whose first row is not behind b.  (The entries are counted, 32 at a time: a
+// search would wait for one after the other.)
 __device__ __forceinline__ int prefix_of(const PrefixAttnArgs &a, int b) {
     if (a.P == 0) return -1;
     if (!a.row_start) return b / (a.B / a.P);
-    int lo = -1, hi = a.P;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.row_start[mid] <= b) lo = mid; else hi = mid;
+    const int lane = threadIdx.x & 31;
+    int starts = 0;
+    for (int p = 0; p <= a.P; p += 32) {
+        const uint64_t at = __ballot(p + lane <= a.P && a.row_start[min(p + lane, a.P)] <= b);
+        starts += __popc((uint32_t)(at >> (threadIdx.x & 32)));
     }
-    return lo >= 0 && b < a.row_start[lo + 1] ? lo : -1;
+    return starts >= 1 && starts <= a.P ? starts - 1 : -1;
 }
 __device__ __forceinline__ int prefix_len(const PrefixAttnArgs &a, int p, int h) {
     return p < 0 ? 0 : a.lens ? min(max(a.lens[(size_t)p * a.H + h], 0), a.cap) : a.cap;
@@ -120,77 +124,74 @@ template <typename T> struct TileLane {
     __device__ __forceinline__ int chunk_bytes(int i) const { return (src_pos ^ KT::swz(row_of(i))) * 16; }
 };
 
-// The rows of a prefix slice from j0 on, j0 + 32 > n: zeros behind the last.
-template <typename T>
-__device__ __forceinline__ void load_prefix_tile(const TileLane<T> &tl, const char *K, const char *V, int j0, int n, u32x4 *kt, u32x4 *vt, int first,
-                                                 int step) {
-    using KT = KeyTile<T>;
-    const char *kb = K + (size_t)j0 * KT::ROWB, *vb = V + (size_t)j0 * KT::ROWB;
-    if (j0 + 32 <= n) {
-#pragma unroll
-        for (int i = 0; i < KT::LOADS; ++i) {
-            if (step > 1 && i % step != first) continue;
-            const uint32_t off = tl.row_of(i) * KT::ROWB + tl.chunk_bytes(i);
-            __builtin_amdgcn_global_load_lds((gptr_t)(kb + off), (lptr_t)(kt + i * WAVE), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((gptr_t)(vb + off), (lptr_t)(vt + i * WAVE), 16, 0, 0);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < KT::LOADS; ++i) {
-            if (step > 1 && i % step != first) continue;
-            const uint32_t off = tl.row_of(i) * KT::ROWB + tl.chunk_bytes(i);
-            const bool there = j0 + tl.row_of(i) < n;
-            const char *ks = there ? kb + off : (const char *)&px_zeros, *vs = there ? vb + off : (const char *)&px_zeros;
-            __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(kt + i * WAVE), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(vt + i * WAVE), 16, 0, 0);
-        }
-    }
-}
-
 // A row's page table, 64 entries at a time, one a lane.
 struct PageWindow {
     const int32_t *table;
-    int first, entry, pages, n_pages;
-    __device__ __forceinline__ PageWindow(const PrefixAttnArgs &a, int b) : table(a.table + (size_t)b * a.max_pages), first(-1), entry(-1),
-                                                                            pages(a.max_pages), n_pages(a.n_pages) {}
-    // entries of pages [lo, hi], hi - lo < 64 (wave-uniform)
-    __device__ __forceinline__ void need(int lo, int hi) {
-        if (first >= 0 && lo >= first && hi < first + 64) return;
+    int first = -(1 << 30), entry = -1, pages, n_pages;
+    __device__ __forceinline__ PageWindow(const PrefixAttnArgs &a, int b) : table(a.table + (size_t)b * a.max_pages), pages(a.max_pages),
+                                                                            n_pages(a.n_pages) {}
+    __device__ __forceinline__ void load(int lo) {
         first = lo;
         const int i = lo + (int)(threadIdx.x & 63);
         entry = i < pages ? table[i] : -1;
         if (entry >= n_pages) entry = -1;
     }
+    // entries of pages [lo, hi], hi - lo < 64 (wave-uniform)
+    __device__ __forceinline__ void need(int lo, int hi) {
+        if (lo < first || hi >= first + 64) load(lo);
+    }
     __device__ __forceinline__ int page(int i) const { return __shfl(entry, i - first, WAVE); }
+    __device__ __forceinline__ int page_uniform(int i) const { return __builtin_amdgcn_readlane(entry, i - first); }   // i the same for the wave
 };
 
-// Tokens [j0, j0 + 32) of a row's pages below n.  Returns which of them are there, one bit each.
-template <typename T>
-__device__ __forceinline__ uint32_t load_tail_tile(const TileLane<T> &tl, const PrefixAttnArgs &a, PageWindow &win, int h, int j0, int n, u32x4 *kt,
-                                                   u32x4 *vt, int first, int step) {
+// Where the 32 rows of a tile are: `base`, the same for the wave, where they follow one another (a prefix, a page that holds all of
+// them), else every lane has the place of row lane % 32.  In rows of the pool or the prefix.
+template <typename T> struct TileRows {
     using KT = KeyTile<T>;
-    const int lane = threadIdx.x & 63;
-    const int shift = a.page_shift, mask = (1 << shift) - 1, last = min(j0 + 31, n - 1);
-    win.need(j0 >> shift, last >> shift);
-    const uint32_t below = n - j0 >= 32 ? 0xFFFFFFFFu : (1u << (n - j0)) - 1;
-    // where the row of token j0 + (lane % 32) begins, in rows of the pool
-    const int j = min(j0 + (lane & 31), last);
-    const int page = win.page(j >> shift);
-    const uint32_t there = (uint32_t)__ballot(page >= 0) & below;
-    const int64_t row = (((int64_t)page * a.H + h) << shift) + (j & mask);
-    const uint32_t lo = (uint32_t)row, hi = (uint32_t)(row >> 32);
-#pragma unroll
-    for (int i = 0; i < KT::LOADS; ++i) {
-        if (step > 1 && i % step != first) continue;
-        const int r = tl.row_of(i);
-        const uint64_t at = (((uint64_t)(uint32_t)__shfl((int)hi, r, WAVE) << 32) | (uint32_t)__shfl((int)lo, r, WAVE)) * KT::ROWB + tl.chunk_bytes(i);
-        const bool ok = (there >> r) & 1;
-        const char *ks = ok ? (const char *)a.Kt + at : (const char *)&px_zeros, *vs = ok ? (const char *)a.Vt + at : (const char *)&px_zeros;
-        __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(kt + i * WAVE), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(vt + i * WAVE), 16, 0, 0);
+    uint64_t base;
+    uint32_t lo, hi, there;                                   // there: which rows are there, one bit each
+    bool in_order;
+    __device__ __forceinline__ uint32_t of_prefix(uint64_t first, int j0, int n) {
+        base = first + j0;
+        there = n - j0 >= 32 ? 0xFFFFFFFFu : (1u << (n - j0)) - 1;
+        in_order = n - j0 >= 32;
+        lo = (uint32_t)(base + (threadIdx.x & 31));
+        hi = (uint32_t)((base + (threadIdx.x & 31)) >> 32);
+        return there;
     }
-    return there;
-}
+    // tokens [j0, j0 + 32) of a row's pages, below n
+    __device__ __forceinline__ uint32_t of_tail(const PrefixAttnArgs &a, PageWindow &win, int h, int j0, int n) {
+        const int shift = a.page_shift, mask = (1 << shift) - 1, last = min(j0 + 31, n - 1);
+        win.need(j0 >> shift, last >> shift);
+        const uint32_t below = n - j0 >= 32 ? 0xFFFFFFFFu : (1u << (n - j0)) - 1;
+        const int j = min(j0 + (int)(threadIdx.x & 31), last);
+        const int page = win.page(j >> shift);
+        there = (uint32_t)__ballot(page >= 0) & below;
+        in_order = shift >= 5 && there == 0xFFFFFFFFu;
+        const uint64_t row = ((uint64_t)((int64_t)page * a.H + h) << shift) + (j & mask);
+        lo = (uint32_t)row;
+        hi = (uint32_t)(row >> 32);
+        base = ((uint64_t)__builtin_amdgcn_readfirstlane(hi) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane(lo);
+        return there;
+    }
+    // the tile of the keys or the values whose row 0 is at `src` -> LDS, asynchronously
+    __device__ __forceinline__ void load(const TileLane<T> &tl, const char *src, u32x4 *tile) const {
+        if (in_order) {
+            const char *first = src + base * KT::ROWB;
+#pragma unroll
+            for (int i = 0; i < KT::LOADS; ++i)
+                __builtin_amdgcn_global_load_lds((gptr_t)(first + (uint32_t)(tl.row_of(i) * KT::ROWB + tl.chunk_bytes(i))), (lptr_t)(tile + i * WAVE), 16, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < KT::LOADS; ++i) {
+                const int r = tl.row_of(i);
+                const uint64_t row = ((uint64_t)(uint32_t)__shfl((int)hi, r, WAVE) << 32) | (uint32_t)__shfl((int)lo, r, WAVE);
+                const char *at = (there >> r) & 1 ? src + row * KT::ROWB + tl.chunk_bytes(i) : (const char *)px_zero_row;
+                __builtin_amdgcn_global_load_lds((gptr_t)at, (lptr_t)(tile + i * WAVE), 16, 0, 0);
+            }
+        }
+    }
+};
 
 // ---- 32 queries of a wave -------------------------------------------------------------------------
 
@@ -329,43 +330,56 @@ template <typename T> struct Queries {
             }
         }
     }
-
-    // One key at a time, for the tiles that values() may not touch (see has_nonfinite): the same state, every lane its own query and half of
-    // the dimensions; a query that does not see the key leaves it out altogether.
-    __device__ __forceinline__ void one_key(const PrefixAttnArgs &a, const T *kr, const T *vr, bool seen) {
-        typedef typename Elem<T>::Raw Raw;
-        const int hf = (threadIdx.x >> 5) & 1;
-        float s = 0.f;
-#pragma unroll
-        for (int f = 0; f < M::FRAGS; ++f) {
-            const u32x4 k = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(kr) + (2 * f + hf) * 16);
-            if constexpr (sizeof(T) == 2) s += RowDot<T>::dot(Raw{k}, Raw{q[f]});
-            else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t ki = k[i], qi = q[f][i];
-                    s = fmaf(__builtin_bit_cast(float, ki), __builtin_bit_cast(float, qi), s);
-                }
-            }
-        }
-        s = (s + other_half(s)) * a.c;
-        if (!seen) return;
-        const float next = fmaxf(m, s), scale = __builtin_amdgcn_exp2f(m - next), w = __builtin_amdgcn_exp2f(s - next);
-        l = l * scale + (hf ? 0.f : w);                       // (the halves' sums are added in the end)
-        m = next;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-            asm volatile("" ::: "memory");                    // (not all the loads at once: they would take the tile loop's registers)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                T v[4];
-                __builtin_memcpy(v, vr + 32 * d + 8 * i + 4 * hf, sizeof(v));
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[d][4 * i + e] = o[d][4 * i + e] * scale + w * (float)v[e];
-            }
-        }
-    }
 };
+
+// One token at a time, for the tiles that values() may not touch (see has_nonfinite): the same state, every lane its own query and half
+// of the dimensions; a query that does not see the token leaves it out altogether.  A call of its own, on a copy of the accumulators in
+// memory: as part of the kernels it took the registers of their loops (8 x 2048 new tokens 2.46 -> 2.97 ms).
+struct LaneState { float o[4][16], m, l; };
+struct TokenSource { const void *K, *V; const int32_t *table; int n_pages, page_shift, H, h; float c; };
+template <typename T>
+static __device__ __attribute__((noinline)) void one_by_one(LaneState *st, TokenSource src, const T *q, int sees, int first, int last)
+{
+    const int hf = (threadIdx.x >> 5) & 1;
+    for (int j = first; j < last; ++j) {
+        const int page = src.table[j >> src.page_shift];
+        if (page < 0 || page >= src.n_pages) continue;
+        const size_t at = ((((size_t)page * src.H + src.h) << src.page_shift) + (j & ((1 << src.page_shift) - 1))) * HEAD_DIM;
+        const T *kr = (const T *)src.K + at + 64 * hf, *vr = (const T *)src.V + at;
+        float s = 0.f;
+#pragma unroll 1
+        for (int f = 0; f < 8; ++f) s += RowDot<T>::dot(Elem<T>::load(kr, f), Elem<T>::load(q + 64 * hf, f));
+        s = (s + other_half(s)) * src.c;
+        if (j >= sees) continue;
+        const float next = fmaxf(st->m, s), scale = __builtin_amdgcn_exp2f(st->m - next), w = __builtin_amdgcn_exp2f(s - next);
+        st->l = st->l * scale + (hf ? 0.f : w);               // (the halves' sums are added in the end)
+        st->m = next;
+#pragma unroll 1
+        for (int d = 0; d < 4; ++d)
+#pragma unroll 1
+            for (int i = 0; i < 16; ++i) st->o[d][i] = st->o[d][i] * scale + w * (float)vr[32 * d + 8 * (i >> 2) + 4 * hf + (i & 3)];
+    }
+}
+// tokens [first, last) of row b for a wave's queries
+template <typename T>
+__device__ __forceinline__ void one_by_one(const PrefixAttnArgs &a, Queries<T> &qs, int b, int h, int first, int last) {
+    LaneState st;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st.o[d][i] = qs.o[d][i];
+    st.m = qs.m;
+    st.l = qs.l;
+    const int64_t HG = a.H * a.G, token = qs.valid ? qs.row / HG : (int64_t)b * a.T, head = qs.valid ? qs.row - token * HG : h * a.G;
+    const TokenSource src = {a.Kt, a.Vt, a.table + (size_t)b * a.max_pages, a.n_pages, a.page_shift, a.H, h, a.c};
+    one_by_one<T>(&st, src, (const T *)a.q + token * a.q_stride + head * HEAD_DIM, qs.valid ? qs.sees : 0, first, last);
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) qs.o[d][i] = st.o[d][i];
+    qs.m = st.m;
+    qs.l = st.l;
+}
 
 // Does the value tile hold an infinity or a NaN?  Where some queries of a tile see a key that others do not (later tokens of the same
 // step), a weight of zero would not keep it out of the others' sums.

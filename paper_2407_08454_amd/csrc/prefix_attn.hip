@@ -74,26 +74,47 @@ __device__ __forceinline__ void store_part(const PrefixAttnArgs &a, const Querie
     }
 }
 
-// What bounds it: the read of the keys and values.  A wave has two stages of 32 keys in LDS, one on its way while it works on the other, so
-// five waves of a compute unit (160 KB of LDS) keep 80 KB in flight; nobody waits for anybody.
+// A query's output from the sum of its weighted values: four dimensions of lane `lane` of 32.
+template <typename T>
+__device__ __forceinline__ void store_out(const PrefixAttnArgs &a, int64_t row, int lane, float top, float total, const f32x4 &sum) {
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    T y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = (T)(sum[i] * inv);
+    __builtin_memcpy((T *)a.out + row * HEAD_DIM + lane * 4, y, sizeof(y));
+    if (a.lse && lane == 0) a.lse[row] = total == 0.f ? -INFINITY : (top + __log2f(total)) * 0.69314718055994531f;
+}
+
+// parts that hold something of a prefix of n states
+__device__ __forceinline__ int parts_of_prefix(const PrefixAttnArgs &a, int n) {
+    const int part = a.wide ? wide_part(n, 0, a.splits_p) * 64 : part_keys(n, max(a.splits_p, 1));
+    return (n + part - 1) / part;
+}
+
+// What bounds it: the read of the keys and values.  A wave has room for one tile of 32 keys and one of their values in LDS: the next keys are
+// asked for as soon as the scores are taken, the next values when they have been added up, so that one of the two is always on its way
+// and mostly both.  Nobody waits for anybody.
 template <typename T>
 __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_split_kernel(PrefixAttnArgs a)
 {
     using KT = KeyTile<T>;
-    __shared__ u32x4 k_a[KT::SLOTS], v_a[KT::SLOTS], k_b[KT::SLOTS], v_b[KT::SLOTS];   // (four objects: see attn_lse_kernel)
+    __shared__ u32x4 kt[KT::SLOTS], vt[KT::SLOTS];           // (two objects: see attn_lse_kernel)
     const int lane = threadIdx.x;
-    const int units_p = a.wide ? 0 : a.tiles_p * a.H * a.splits_p;
+    // the tails first: their keys are found by way of lengths and page table, and they may be the longer ones
+    const int units_t = a.stream ? 0 : a.B * a.tiles_t * a.H * a.splits_t;
     int u = blockIdx.x;
-    const bool tail = u >= units_p;
+    const bool tail = u < units_t;
+    PageWindow win(a, 0);
     int h, s, b = 0, p = -1, j0, end, least = 0;              // least: tokens that every query of the tile sees
     int64_t lin, lin_end;
     if (!tail) {
+        u -= units_t;
         // the query tiles of a part read the same keys: on one XCD
         const int groups = a.H * a.splits_p;
         int group, tile;
         if (groups % 8 == 0) {
             const int slot = u >> 3;
-            group = slot / a.tiles_p * 8 + (u & 7);
+            group = slot / a.tiles_p * 8 + (blockIdx.x & 7);
             tile = slot % a.tiles_p;
         } else {
             group = u / a.tiles_p;
@@ -110,13 +131,14 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
         j0 = s * part;
         end = min(n, j0 + part);
     } else {
-        u -= units_p;
         s = u % a.splits_t;
         u /= a.splits_t;
         const int tile = u % a.tiles_t;
         u /= a.tiles_t;
         h = u % a.H;
         b = u / a.H;
+        win = PageWindow(a, b);
+        win.load(0);                                          // (on its way with the lengths)
         const int n_new = clamp_len(a.new_lens, b, a.T), n = tail_len(a, b), part = part_keys(n, a.splits_t);
         const int64_t row_lin = (int64_t)b * a.T * a.G;
         lin = row_lin + (int64_t)tile * PX_QUERIES;
@@ -131,60 +153,41 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
 
     const TileLane<T> tl(lane);
     Queries<T> qs;
-    const char *Kp = nullptr, *Vp = nullptr;
-    PageWindow win(a, b);
-    if (!tail) {
-        const size_t at = ((size_t)p * a.H + h) * a.cap * KT::ROWB;
-        Kp = (const char *)a.Kp + at;
-        Vp = (const char *)a.Vp + at;
-    }
-    auto load = [&](int j, u32x4 *kt, u32x4 *vt) -> uint32_t {
-        if (tail) return load_tail_tile<T>(tl, a, win, h, j, end, kt, vt, 0, 1);
-        load_prefix_tile<T>(tl, Kp, Vp, j, end, kt, vt, 0, 1);
-        return end - j >= 32 ? 0xFFFFFFFFu : (1u << (end - j)) - 1;
+    TileRows<T> rows;                                        // of the tile that is loaded next
+    const auto find = [&](int j) -> uint32_t {
+        if (tail) return rows.of_tail(a, win, h, j, end);
+        return rows.of_prefix(((size_t)p * a.H + h) * a.cap, j, end);
     };
+    const char *K = (const char *)(tail ? a.Kt : a.Kp), *V = (const char *)(tail ? a.Vt : a.Vp);
+    uint32_t next = find(j0);
+    rows.load(tl, K, kt);
+    rows.load(tl, V, vt);
+    qs.init(a, lin + (lane & 31), lin_end, h);
     int stop = end;                                          // tokens from here on one at a time
-    auto work = [&](int j, uint32_t there, const u32x4 *kt, const u32x4 *vt) {
+    for (int j = j0; j < end; j += 32) {
+        const uint32_t there = next;
+        wait_vmcnt<KT::LOADS>();
         f32x16 x = qs.scores(tl, kt);
+        wait_lds();
+        if (j + 32 < end) {
+            next = find(j + 32);
+            rows.load(tl, K, kt);
+            wait_vmcnt<KT::LOADS>();
+        } else {
+            wait_vmcnt<0>();
+        }
         const bool mixed = tail && j + 32 > least;
         if (mixed || there != 0xFFFFFFFFu) {
             qs.mask(x, there, tail ? qs.sees - j : 32);
-            if (mixed && a.T > 1 && has_nonfinite<T>(vt)) { stop = j; return; }
+            if (mixed && a.T > 1 && has_nonfinite<T>(vt)) { stop = j; break; }
         }
         qs.weights(x, a.c);
         qs.values(tl, x, vt);
-    };
-    uint32_t there_a = load(j0, k_a, v_a), there_b = 0;
-    qs.init(a, lin + (lane & 31), lin_end, h);
-    for (int j = j0;;) {
-        if (j + 32 < end) {
-            wait_lds();
-            there_b = load(j + 32, k_b, v_b);
-            wait_vmcnt<2 * KT::LOADS>();
-        } else {
-            wait_vmcnt<0>();
-        }
-        work(j, there_a, k_a, v_a);
-        j += 32;
-        if (j >= end || stop < end) break;
-        if (j + 32 < end) {
-            wait_lds();
-            there_a = load(j + 32, k_a, v_a);
-            wait_vmcnt<2 * KT::LOADS>();
-        } else {
-            wait_vmcnt<0>();
-        }
-        work(j, there_b, k_b, v_b);
-        j += 32;
-        if (j >= end || stop < end) break;
+        wait_lds();
+        if (j + 32 < end) rows.load(tl, V, vt);
     }
     wait_vmcnt<0>();
-    for (int j = stop; j < end; ++j) {                       // (tails only)
-        const int page = a.table[(size_t)b * a.max_pages + (j >> a.page_shift)];
-        if (page < 0 || page >= a.n_pages) continue;
-        const size_t at = ((((size_t)page * a.H + h) << a.page_shift) + (j & ((1 << a.page_shift) - 1))) * HEAD_DIM;
-        qs.one_key(a, (const T *)a.Kt + at, (const T *)a.Vt + at, j < qs.sees);
-    }
+    if (stop < end) one_by_one<T>(a, qs, b, h, stop, end);   // (tails only)
 
     const float l = qs.l + other_half(qs.l);
     if (!qs.valid) return;
@@ -232,7 +235,7 @@ template <typename T> struct WideLoad {
             for (int i = 0; i < N; ++i) {
                 const uint32_t at = (32 * s + row[i]) * KT::ROWB + off[i];
                 const bool ok = j0 + 32 * s + row[i] < n;
-                const char *ks = ok ? kb + at : (const char *)&px_zeros, *vs = ok ? vb + at : (const char *)&px_zeros;
+                const char *ks = ok ? kb + at : (const char *)px_zero_row, *vs = ok ? vb + at : (const char *)px_zero_row;
                 __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(kt + s * KT::SLOTS + (slot + i) * WAVE), 16, 0, 0);
                 __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(vt + s * KT::SLOTS + (slot + i) * WAVE), 16, 0, 0);
             }
@@ -253,7 +256,7 @@ template <typename T> struct WideLoad {
                 const int r = 32 * s + row[i];
                 const uint64_t at = (((uint64_t)(uint32_t)__shfl((int)hi, r, WAVE) << 32) | (uint32_t)__shfl((int)lo, r, WAVE)) * KT::ROWB + off[i];
                 const bool ok = (there >> r) & 1;
-                const char *ks = ok ? (const char *)a.Kt + at : (const char *)&px_zeros, *vs = ok ? (const char *)a.Vt + at : (const char *)&px_zeros;
+                const char *ks = ok ? (const char *)a.Kt + at : (const char *)px_zero_row, *vs = ok ? (const char *)a.Vt + at : (const char *)px_zero_row;
                 __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(kt + s * KT::SLOTS + (slot + i) * WAVE), 16, 0, 0);
                 __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(vt + s * KT::SLOTS + (slot + i) * WAVE), 16, 0, 0);
             }
@@ -353,14 +356,7 @@ __global__ __launch_bounds__(4 * WAVE, 2) void prefix_attn_wide_kernel(PrefixAtt
             if (++v >= v_end) break;
         }
     }
-    if (ROWS && !idle) {
-        for (int j = stop; j < tail_end; ++j) {
-            const int page = a.table[(size_t)b * a.max_pages + (j >> a.page_shift)];
-            if (page < 0 || page >= a.n_pages) continue;
-            const size_t at = ((((size_t)page * a.H + h) << a.page_shift) + (j & ((1 << a.page_shift) - 1))) * HEAD_DIM;
-            qs.one_key(a, (const T *)a.Kt + at, (const T *)a.Vt + at, j < qs.sees);
-        }
-    }
+    if (ROWS && !idle && stop < tail_end) one_by_one<T>(a, qs, b, h, stop, tail_end);
     const float l = qs.l + other_half(qs.l);
     if (!qs.valid) return;
     if (ROWS && splits == 1) {
@@ -381,67 +377,341 @@ __global__ __launch_bounds__(4 * WAVE, 2) void prefix_attn_wide_kernel(PrefixAtt
     store_part(a, qs, (size_t)qs.row * (splits + a.splits_t) + part, l);
 }
 
-// 32 lanes a query row, four dimensions each.
-template <typename T>
+// ---- a few queries -------------------------------------------------------------------------------
+
+// Up to NQ queries of one row (its T * G) over a part of its tail, or of its prefix, by a workgroup: rows go straight from memory into
+// registers, sixteen lanes a row, and the matrix cores have nothing to offer.  What bounds it: the read of the keys and values.  A lane
+// keeps KEYS keys and values on their way, the next keys while values are added up, the next values while scores are taken.
+//   a.splits_t tail parts a row, then, with PX_STREAM_ALL, a.splits_p parts of its prefix (a prefix that several rows share is
+//   better read by the kernels above, once for all).
+// A tail in one part whose prefix parts an earlier launch has left is joined with them here (PX_STREAM_JOIN).
+template <typename T, int NQ>
+struct StreamState {
+    float m[NQ], l[NQ], acc[NQ][8];
+};
+
+// an operation over the four 16-lane rows of a wave, every lane gets the result
+template <typename F> __device__ __forceinline__ float rows4_all(float v, F op) {
+    const uint32_t x = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    const uint32_t r0 = r[0], r1 = r[1];
+    const uint32_t y = __builtin_bit_cast(uint32_t, op(__builtin_bit_cast(float, r0), __builtin_bit_cast(float, r1)));
+    const auto t = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+    const uint32_t t0 = t[0], t1 = t[1];
+    return op(__builtin_bit_cast(float, t0), __builtin_bit_cast(float, t1));
+}
+
+template <typename T, int NQ>
+__global__ __launch_bounds__(4 * WAVE, NQ <= 2 ? 3 : 2) void prefix_attn_stream_kernel(PrefixAttnArgs a)
+{
+    typedef typename Elem<T>::Raw Raw;
+    constexpr int WAVES = 4, KEYS = (NQ == 8 ? 4 : 8) / (sizeof(T) / 2), STEP = 4 * KEYS, ROUND = WAVES * STEP;   // keys of a lane, a wave, the workgroup
+    __shared__ float acc_of[WAVES][NQ][HEAD_DIM], m_of[WAVES][NQ], l_of[WAVES][NQ];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane16 = lane & 15, sub = lane >> 4;
+    const int units_t = a.B * a.H * a.splits_t;
+    int u = blockIdx.x;
+    const bool tail = u < units_t;
+    const int splits = tail ? a.splits_t : a.splits_p;
+    if (!tail) u -= units_t;
+    const int s = u % splits;
+    u /= splits;
+    const int h = u % a.H, b = u / a.H;
+    PageWindow win(a, b);
+    if (tail) win.load(0);                                    // (on its way with the lengths)
+    const int n_new = clamp_len(a.new_lens, b, a.T), n_tail = tail_len(a, b);
+    const int nq = n_new * a.G;
+    if (nq == 0) return;
+    const int p = tail && a.stream != PX_STREAM_JOIN ? -1 : prefix_of(a, b);
+    const int n = tail ? n_tail : prefix_len(a, p, h), part = part_keys(n, splits);
+    const int j0 = s * part, end = min(n, j0 + part);
+    if (j0 >= end && !(tail && a.stream == PX_STREAM_JOIN)) return;
+
+    const int64_t token0 = (int64_t)b * a.T;
+    Raw q[NQ];
+    int sees[NQ];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+        const int t = min(i, nq - 1) / a.G, g = min(i, nq - 1) - t * a.G;
+        q[i] = Elem<T>::load((const T *)a.q + (token0 + t) * a.q_stride + (int64_t)(h * a.G + g) * HEAD_DIM, lane16);
+        sees[i] = tail ? min(max(n_tail - n_new + t + 1, 0), n_tail) : n;
+    }
+    const int least = sees[0];
+    StreamState<T, NQ> st;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+        st.m[i] = PX_NONE;
+        st.l[i] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) st.acc[i][e] = 0.f;
+    }
+    const size_t prefix_row = ((size_t)max(p, 0) * a.H + h) * a.cap;
+    // keys j + 4 i + sub of the wave: their rows, in elements of the pool or the prefix; negative where there is none
+    const auto row_of = [&](int j, int i) -> int64_t {
+        const int k = j + 4 * i + sub;
+        if (!tail) return k < end ? (int64_t)(prefix_row + k) : -1;
+        const int at = min(k, end - 1), page = win.page(at >> a.page_shift);
+        return k < end && page >= 0 ? (((int64_t)page * a.H + h) << a.page_shift) + (at & ((1 << a.page_shift) - 1)) : -1;
+    };
+    const char *Kb = (const char *)(tail ? a.Kt : a.Kp), *Vb = (const char *)(tail ? a.Vt : a.Vp);
+    constexpr int ROWB = HEAD_DIM * (int)sizeof(T);
+    const uint32_t in_four = sub * ROWB;                      // (four neighbouring rows a load: of one page, where pages have four tokens)
+    Raw kr[KEYS], vr[KEYS];
+    // keys or values [j, j + STEP) of the wave; returns which of this lane's are there
+    const auto load = [&](const char *base, int j, Raw *r) -> uint32_t {
+        uint32_t there = 0;
+        if (j + STEP <= end && (!tail || a.page_shift >= 2)) {
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i) {
+                const char *four = base + (prefix_row + j + 4 * i) * ROWB;
+                bool ok = true;
+                if (tail) {
+                    const int page = win.page_uniform((j + 4 * i) >> a.page_shift);
+                    ok = page >= 0;
+                    four = ok ? base + (size_t)((((int64_t)page * a.H + h) << a.page_shift) + ((j + 4 * i) & ((1 << a.page_shift) - 1))) * ROWB
+                              : (const char *)px_zero_row;
+                }
+                r[i] = Elem<T>::load_stream((const T *)(four + in_four), lane16);
+                there |= (uint32_t)ok << i;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i) {
+                const int64_t row = row_of(j, i);
+                r[i] = Elem<T>::load_stream((const T *)(row >= 0 ? base + row * ROWB : (const char *)px_zero_row), lane16);
+                there |= (uint32_t)(row >= 0) << i;
+            }
+        }
+        return there;
+    };
+    const auto need = [&](int j) { if (tail) win.need(j >> a.page_shift, (min(j + STEP, end) - 1) >> a.page_shift); };
+    uint32_t there = 0;
+    int j = j0 + wave * STEP;
+    if (j < end) {
+        need(j);
+        there = load(Kb, j, kr);
+        load(Vb, j, vr);
+    }
+    for (; j < end; j += ROUND) {
+        float x[NQ][KEYS];
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i)
+#pragma unroll
+            for (int k = 0; k < NQ; ++k) x[k][i] = row16_sum(RowDot<T>::dot(kr[i], q[k])) * a.c;
+        const bool more = j + ROUND < end;
+        const bool mixed = a.T > 1 && tail && j + STEP > least;
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i)
+#pragma unroll
+            for (int k = 0; k < NQ; ++k)
+                if (!((there >> i) & 1) || (mixed && j + 4 * i + sub >= sees[k])) x[k][i] = -INFINITY;
+        if (more) {
+            need(j + ROUND);
+            there = load(Kb, j + ROUND, kr);
+        }
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) {
+            float top = x[k][0];
+#pragma unroll
+            for (int i = 1; i < KEYS; ++i) top = fmaxf(top, x[k][i]);
+            top = fmaxf(top, st.m[k]);
+            const float scale = __builtin_amdgcn_exp2f(st.m[k] - top);
+            st.m[k] = top;
+            st.l[k] *= scale;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) st.acc[k][e] *= scale;
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i) {
+                x[k][i] = __builtin_amdgcn_exp2f(x[k][i] - top);
+                st.l[k] += x[k][i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            float v[8];
+            Elem<T>::to_float(vr[i], v);
+#pragma unroll
+            for (int k = 0; k < NQ; ++k) {
+                if (mixed) {                                  // (a value that the query does not see may be infinite)
+                    const bool seen = j + 4 * i + sub < sees[k];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) st.acc[k][e] = seen ? fmaf(x[k][i], v[e], st.acc[k][e]) : st.acc[k][e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) st.acc[k][e] = fmaf(x[k][i], v[e], st.acc[k][e]);
+                }
+            }
+        }
+        if (more) load(Vb, j + ROUND, vr);
+    }
+    // the four rows of the wave, then the four waves
+#pragma unroll
+    for (int k = 0; k < NQ; ++k) {
+        const float top = rows4_all(st.m[k], [](float x, float y) { return fmaxf(x, y); });
+        const float scale = __builtin_amdgcn_exp2f(st.m[k] - top), l = rows4_sum(st.l[k] * scale);
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = rows4_sum(st.acc[k][e] * scale);
+        if (sub == 0) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc_of[wave][k][lane16 * 8 + e] = y[e];
+        }
+        if (lane == 0) { m_of[wave][k] = top; l_of[wave][k] = l; }
+    }
+    __syncthreads();
+    // 32 lanes a query, four dimensions each; where prefix parts are joined, as many such groups a query as there are for them
+    const int lane32 = threadIdx.x & 31, slot = threadIdx.x >> 5;
+    constexpr int PER = 2 * WAVES / NQ;                       // groups a query
+    const int k = slot / PER, r = slot % PER;
+    const int t = k / a.G, g = k - t * a.G;
+    const int64_t row = (token0 + t) * (a.H * a.G) + h * a.G + g;
+    const size_t first = (size_t)row * (a.splits_p + a.splits_t);
+    const bool join = tail && a.stream == PX_STREAM_JOIN;
+    float top = PX_NONE, total = 0.f;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    const auto add = [&](float m, float l, const f32x4 &v) {
+        const float next = fmaxf(top, m), before = __builtin_amdgcn_exp2f(top - next), scale = __builtin_amdgcn_exp2f(m - next);
+        total = total * before + l * scale;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] = sum[e] * before + v[e] * scale;
+        top = next;
+    };
+    if (k < nq && join) {
+        const int used = parts_of_prefix(a, prefix_len(a, p, h));
+#pragma unroll 4
+        for (int i = r; i < used; i += PER)
+            add(a.stat[2 * (first + i)], a.stat[2 * (first + i) + 1], *reinterpret_cast<const f32x4 *>(a.part + (first + i) * HEAD_DIM + lane32 * 4));
+    }
+    if (k < nq && r == 0) {
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) add(m_of[w][k], l_of[w][k], *reinterpret_cast<const f32x4 *>(&acc_of[w][k][lane32 * 4]));
+    }
+    if (join && PER > 1) {
+        __shared__ f32x4 sum_of[2 * WAVES][32];
+        __shared__ float top_of[2 * WAVES], total_of[2 * WAVES];
+        sum_of[slot][lane32] = sum;
+        if (lane32 == 0) { top_of[slot] = top; total_of[slot] = total; }
+        __syncthreads();
+        if (r == 0) {
+#pragma unroll
+            for (int i = 1; i < PER; ++i) add(top_of[slot + i], total_of[slot + i], sum_of[slot + i][lane32]);
+        }
+    }
+    if (k >= nq || r != 0) return;
+    if (join) {
+        store_out<T>(a, row, lane32, top, total, sum);
+    } else {
+        const size_t at = first + (tail ? a.splits_p + s : s);
+        *reinterpret_cast<f32x4 *>(a.part + at * HEAD_DIM + lane32 * 4) = sum;
+        if (lane32 == 0) { a.stat[2 * at] = top; a.stat[2 * at + 1] = total; }
+    }
+}
+
+// ---- joining ---------------------------------------------------------------------------------------
+
+// The parts of a query: GROUPS groups of 32 lanes a query row, four dimensions a lane, the parts dealt to the groups.  Bound by the way of
+// a few bytes through the memory: each group's first JOIN_AHEAD parts are on their way before it is known which of them there are.
+constexpr int JOIN_AHEAD = 4;
+template <typename T, int GROUPS>
 __global__ __launch_bounds__(PX_JOIN_ROWS * 32) void prefix_attn_join_kernel(PrefixAttnArgs a)
 {
-    const int HG = a.H * a.G, lane = threadIdx.x & 31;
-    const int64_t row = (int64_t)blockIdx.x * PX_JOIN_ROWS + (threadIdx.x >> 5);
+    __shared__ f32x4 sum_of[PX_JOIN_ROWS][32];
+    __shared__ float top_of[PX_JOIN_ROWS], total_of[PX_JOIN_ROWS];
+    const int HG = a.H * a.G, lane = threadIdx.x & 31, slot = threadIdx.x >> 5, g = slot % GROUPS;
+    const int64_t row = (int64_t)blockIdx.x * (PX_JOIN_ROWS / GROUPS) + slot / GROUPS;
     const int64_t token = row / HG;
     const int b = (int)(token / a.T), t = (int)(token - (int64_t)b * a.T), h = (int)(row - token * HG) / a.G;
-    if (b >= a.B) return;
-    const int n_new = clamp_len(a.new_lens, b, a.T);
-    if (t >= n_new) return;
-    const int n = prefix_len(a, prefix_of(a, b), h), n_tail = tail_len(a, b), sees = min(max(n_tail - n_new + t + 1, 0), n_tail);
-    int used_p, used;
-    if (a.wide == PX_WIDE_ROWS) {
-        const int part = wide_part(n, n_tail, a.splits_p);
-        used_p = used = (((n + 63) >> 6) + ((sees + 63) >> 6) + part - 1) / part;
-    } else {
-        if (a.wide == PX_WIDE_PREFIX) {
-            const int part = wide_part(n, 0, a.splits_p);
-            used_p = (((n + 63) >> 6) + part - 1) / part;
-        } else {
-            const int part = part_keys(n, max(a.splits_p, 1));
-            used_p = (n + part - 1) / part;
-        }
-        const int part_t = part_keys(n_tail, max(a.splits_t, 1));
-        used = used_p + (sees + part_t - 1) / part_t;
-    }
-    const size_t first = (size_t)row * (a.splits_p + a.splits_t);
-    const auto slot = [&](int k) { return first + (k < used_p ? k : a.splits_p + k - used_p); };
-    float top = PX_NONE;
-    for (int k = lane; k < used; k += 32) top = fmaxf(top, a.stat[2 * slot(k)]);
+    const int parts = a.splits_p + a.splits_t;
+    const size_t first = (size_t)row * parts;
+    const bool there = b < a.B;
+    f32x4 v[JOIN_AHEAD];
+    float m[JOIN_AHEAD], l[JOIN_AHEAD];
 #pragma unroll
-    for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d, 32));
+    for (int i = 0; i < JOIN_AHEAD; ++i) {
+        const int k = g + GROUPS * i;
+        if (there && k < parts) {
+            m[i] = a.stat[2 * (first + k)];
+            l[i] = a.stat[2 * (first + k) + 1];
+            v[i] = *reinterpret_cast<const f32x4 *>(a.part + (first + k) * HEAD_DIM + lane * 4);
+        }
+    }
+    int used_p = 0, used_t = 0;
+    bool valid = false;
+    if (there) {
+        const int n_new = clamp_len(a.new_lens, b, a.T);
+        valid = t < n_new;
+        const int n = prefix_len(a, prefix_of(a, b), h), n_tail = tail_len(a, b), sees = min(max(n_tail - n_new + t + 1, 0), n_tail);
+        if (a.wide == PX_WIDE_ROWS) {
+            const int part = wide_part(n, n_tail, a.splits_p);
+            used_p = (((n + 63) >> 6) + ((sees + 63) >> 6) + part - 1) / part;
+        } else {
+            used_p = parts_of_prefix(a, n);
+            const int part_t = part_keys(n_tail, max(a.splits_t, 1));
+            used_t = (sees + part_t - 1) / part_t;
+        }
+    }
+    const auto used = [&](int k) { return k < a.splits_p ? k < used_p : k - a.splits_p < used_t; };
+    float top = PX_NONE;
+#pragma unroll
+    for (int i = 0; i < JOIN_AHEAD; ++i) {
+        const int k = g + GROUPS * i;
+        if (valid && k < parts && used(k)) top = fmaxf(top, m[i]);
+        else m[i] = PX_NONE, l[i] = 0.f, v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     float total = 0.f;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int k = 0; k < used; ++k) {
-        const size_t at = slot(k);
-        const float scale = __builtin_amdgcn_exp2f(a.stat[2 * at] - top);
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(a.part + at * HEAD_DIM + lane * 4);
-        total += a.stat[2 * at + 1] * scale;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] += v[i] * scale;
+    for (int i = 0; i < JOIN_AHEAD; ++i) {
+        const float scale = __builtin_amdgcn_exp2f(m[i] - top);
+        total += l[i] * scale;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += v[i][e] * scale;
     }
-    const float inv = total == 0.f ? 0.f : 1.f / total;
-    T *dst = (T *)a.out + row * HEAD_DIM + lane * 4;
-    T y[4];
+    if (valid) {
+        for (int k = g + GROUPS * JOIN_AHEAD; k < parts; k += GROUPS) {
+            if (k >= used_p && k < a.splits_p) { k += (a.splits_p - 1 - k) / GROUPS * GROUPS; continue; }
+            if (!used(k)) { if (k >= a.splits_p) break; continue; }
+            const float mk = a.stat[2 * (first + k)], lk = a.stat[2 * (first + k) + 1];
+            const f32x4 vk = *reinterpret_cast<const f32x4 *>(a.part + (first + k) * HEAD_DIM + lane * 4);
+            const float next = fmaxf(top, mk), before = __builtin_amdgcn_exp2f(top - next), scale = __builtin_amdgcn_exp2f(mk - next);
+            total = total * before + lk * scale;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = (T)(sum[i] * inv);
-    __builtin_memcpy(dst, y, sizeof(y));
-    if (a.lse && lane == 0) a.lse[row] = total == 0.f ? -INFINITY : (top + __log2f(total)) * 0.69314718055994531f;
+            for (int e = 0; e < 4; ++e) sum[e] = sum[e] * before + vk[e] * scale;
+            top = next;
+        }
+    }
+    if constexpr (GROUPS > 1) {
+        sum_of[slot][lane] = sum;
+        if (lane == 0) { top_of[slot] = top; total_of[slot] = total; }
+        __syncthreads();
+        if (g != 0) return;
+        float all = top;
+#pragma unroll
+        for (int i = 1; i < GROUPS; ++i) all = fmaxf(all, top_of[slot + i]);
+        const float own = __builtin_amdgcn_exp2f(top - all);
+        total *= own;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] *= own;
+#pragma unroll
+        for (int i = 1; i < GROUPS; ++i) {
+            const float scale = __builtin_amdgcn_exp2f(top_of[slot + i] - all);
+            const f32x4 vi = sum_of[slot + i][lane];
+            total += total_of[slot + i] * scale;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += vi[e] * scale;
+        }
+        top = all;
+    }
+    if (valid) store_out<T>(a, row, lane, top, total, sum);
 }
 
 // ---- host side ------------------------------------------------------------------------------------
 
-// Parts of a list of keys that is `most` long at most, `units` of them at a time: enough that every compute unit has five waves, of 64 keys each
+// Parts of a list of keys that is `most` long at most, `units` of them at a time: as many as fill the chip's `slots` once, of `least` keys each
 // at least; where there is more to read, four times as many, of 512 each, so that the last ones to end leave little of the chip idle.
-static int parts_for(int64_t units, int64_t most)
+static int parts_for(int64_t units, int64_t most, int64_t slots, int64_t least)
 {
     if (units <= 0 || most <= 0) return 0;
-    const int64_t one_round = std::min<int64_t>(1280 / units, most / 64), rounds = std::min<int64_t>(5120 / units, most / 512);
+    const int64_t one_round = std::min<int64_t>(slots / units, most / least), rounds = std::min<int64_t>(4 * slots / units, most / 512);
     return (int)std::max<int64_t>(1, std::max(one_round, rounds));
 }
 
@@ -478,13 +748,26 @@ static void plan(const kvm_shape &sh, const kvm_prefix *prefix, const kvm_pages 
             a.splits_p = (int)std::max<int64_t>(1, std::min<int64_t>(512 / wide_prompts, a.cap / 256));
         }
     }
+    a.stream = per_row <= 8 && a.table ? (a.P && a.B > a.P ? PX_STREAM_TAILS : PX_STREAM_ALL) : PX_STREAM_NONE;
+    if (per_row <= 8 && a.P && a.B <= a.P) a.stream = PX_STREAM_ALL;
+    if (a.stream == PX_STREAM_ALL) {
+        // a row's prefix and tail are worked on at the same time: both of them fill the chip
+        a.splits_p = a.P ? parts_for((int64_t)a.B * a.H, a.cap, 512, 128) : 0;
+        a.splits_t = a.table ? parts_for((int64_t)a.B * a.H, tail_most, 512, 128) : 0;
+        a.wide = PX_WIDE_NONE;
+        if (a.splits_p == 0 && a.splits_t == 1) a.stream = PX_STREAM_JOIN;   // nothing to join: it writes the output itself
+        return;
+    }
     if (a.P && !a.wide) {
         a.tiles_p = tiles_of_prompts(a, PX_QUERIES);
-        a.splits_p = parts_for((a.B * per_row + PX_QUERIES - 1) / PX_QUERIES * a.H, a.cap);
+        a.splits_p = parts_for((a.B * per_row + PX_QUERIES - 1) / PX_QUERIES * a.H, a.cap, 1024, 64);
     }
-    if (a.table) {
+    if (a.stream) {
+        a.splits_t = parts_for((int64_t)a.B * a.H, tail_most, 512, 128);
+        if (a.splits_t == 1) a.stream = PX_STREAM_JOIN;
+    } else if (a.table) {
         a.tiles_t = (int)((per_row + PX_QUERIES - 1) / PX_QUERIES);
-        a.splits_t = parts_for((int64_t)a.B * a.tiles_t * a.H, tail_most);
+        a.splits_t = parts_for((int64_t)a.B * a.tiles_t * a.H, tail_most, 1024, 64);
     }
 }
 
@@ -512,16 +795,38 @@ static kvm_status launch_t(const PrefixAttnArgs &a, hipStream_t st)
             if (rc != KVM_OK || direct(a)) return rc;
         }
     }
-    const int64_t units = a.wide == PX_WIDE_ROWS ? 0 : (a.wide ? 0 : (int64_t)a.tiles_p * a.H * a.splits_p) + (int64_t)a.B * a.tiles_t * a.H * a.splits_t;
+    int64_t units = 0;
+    if (!a.wide && a.stream != PX_STREAM_ALL) units += (int64_t)a.tiles_p * a.H * a.splits_p;
+    if (a.wide != PX_WIDE_ROWS && !a.stream) units += (int64_t)a.B * a.tiles_t * a.H * a.splits_t;
     if (units > 0) {
         ProfScope prof("prefix_attn_split_kernel", st);
         hipLaunchKernelGGL(prefix_attn_split_kernel<T>, dim3((unsigned)units), dim3(WAVE), 0, st, a);
         rc = check_launch("prefix_attn_split_kernel");
         if (rc != KVM_OK) return rc;
     }
+    if (a.stream) {
+        const int64_t blocks = (int64_t)a.B * a.H * (a.splits_t + (a.stream == PX_STREAM_ALL ? a.splits_p : 0));
+        const auto stream = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(4 * WAVE), 0, st, a); };
+        ProfScope prof("prefix_attn_stream_kernel", st);
+        switch (a.T * a.G) {
+        case 1: stream(prefix_attn_stream_kernel<T, 1>); break;
+        case 2: stream(prefix_attn_stream_kernel<T, 2>); break;
+        case 3: case 4: stream(prefix_attn_stream_kernel<T, 4>); break;
+        default: stream(prefix_attn_stream_kernel<T, 8>);
+        }
+        rc = check_launch("prefix_attn_stream_kernel");
+        if (rc != KVM_OK || a.stream == PX_STREAM_JOIN) return rc;
+    }
     ProfScope prof("prefix_attn_join_kernel", st);
-    hipLaunchKernelGGL(prefix_attn_join_kernel<T>, dim3((unsigned)((query_rows(a) + PX_JOIN_ROWS - 1) / PX_JOIN_ROWS)), dim3(PX_JOIN_ROWS * 32), 0,
-                       st, a);
+    const auto join = [&](auto kernel, int groups) {
+        const int rows = PX_JOIN_ROWS / groups;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((query_rows(a) + rows - 1) / rows)), dim3(PX_JOIN_ROWS * 32), 0, st, a);
+    };
+    const int parts = a.splits_p + a.splits_t;
+    if (parts <= JOIN_AHEAD) join(prefix_attn_join_kernel<T, 1>, 1);
+    else if (parts <= 2 * JOIN_AHEAD) join(prefix_attn_join_kernel<T, 2>, 2);
+    else if (parts <= 4 * JOIN_AHEAD) join(prefix_attn_join_kernel<T, 4>, 4);
+    else join(prefix_attn_join_kernel<T, 8>, 8);
     return check_launch("prefix_attn_join_kernel");
 }
 
