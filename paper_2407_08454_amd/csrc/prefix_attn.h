@@ -16,7 +16,6 @@ namespace kvm {
 constexpr float PX_NONE = -3.0e38f;      // maximum of no score: finite, so that no inf - inf arises
 constexpr float PX_SLACK = 8.f;          // weights may reach 2^8 before a query's accumulators are put on a new maximum
 
-enum { PX_STREAM_NONE = 0, PX_STREAM_TAILS = 1, PX_STREAM_JOIN = 2, PX_STREAM_ALL = 3 };
 enum { PX_WIDE_NONE = 0, PX_WIDE_ROWS = 1, PX_WIDE_PREFIX = 2 };
 
 struct PrefixAttnArgs {
@@ -30,13 +29,13 @@ struct PrefixAttnArgs {
     int tiles_p, tiles_t;                 // query tiles of all prompts (an upper bound with row_start), of one row
     int splits_p, splits_t;               // parts that a prefix and a tail are split into
     int wide;                             // which of the keys go to 128 queries at a time (PX_WIDE_*)
-    int stream;                           // which of the keys go to the few queries of a row (PX_STREAM_*)
+    int stream_p, stream_t;               // prefixes and tails of so many keys are read with the non-temporal hint
     float c;                              // log2(e) / sqrt(d): scores in base 2
 };
 
-// Four rows of zeros that stand for the rows behind a tile's last key and for missing pages: a key that nobody sees must not bring
+// 16 bytes of zeros that stand for the rows behind a tile's last key and for missing pages: a key that nobody sees must not bring
 // what lies in its memory into a product, where even a weight of zero would not take a NaN away.
-static __device__ const u32x4 px_zero_row[4 * HEAD_DIM * sizeof(float) / 16] = {};
+static __device__ const u32x4 px_zeros = {0u, 0u, 0u, 0u};
 
 // The prompt of row b, or -1, b the same for 32 lanes: the last whose first row is not behind b.  (The entries are counted, 32 at a time: a
 // search would wait for one after the other.)
@@ -141,7 +140,6 @@ struct PageWindow {
         if (lo < first || hi >= first + 64) load(lo);
     }
     __device__ __forceinline__ int page(int i) const { return __shfl(entry, i - first, WAVE); }
-    __device__ __forceinline__ int page_uniform(int i) const { return __builtin_amdgcn_readlane(entry, i - first); }   // i the same for the wave
 };
 
 // Where the 32 rows of a tile are: `base`, the same for the wave, where they follow one another (a prefix, a page that holds all of
@@ -175,19 +173,19 @@ template <typename T> struct TileRows {
         return there;
     }
     // the tile of the keys or the values whose row 0 is at `src` -> LDS, asynchronously
-    __device__ __forceinline__ void load(const TileLane<T> &tl, const char *src, u32x4 *tile) const {
+    template <int HINT> __device__ __forceinline__ void load(const TileLane<T> &tl, const char *src, u32x4 *tile) const {
         if (in_order) {
             const char *first = src + base * KT::ROWB;
 #pragma unroll
             for (int i = 0; i < KT::LOADS; ++i)
-                __builtin_amdgcn_global_load_lds((gptr_t)(first + (uint32_t)(tl.row_of(i) * KT::ROWB + tl.chunk_bytes(i))), (lptr_t)(tile + i * WAVE), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((gptr_t)(first + (uint32_t)(tl.row_of(i) * KT::ROWB + tl.chunk_bytes(i))), (lptr_t)(tile + i * WAVE), 16, 0, HINT);
         } else {
 #pragma unroll
             for (int i = 0; i < KT::LOADS; ++i) {
                 const int r = tl.row_of(i);
                 const uint64_t row = ((uint64_t)(uint32_t)__shfl((int)hi, r, WAVE) << 32) | (uint32_t)__shfl((int)lo, r, WAVE);
-                const char *at = (there >> r) & 1 ? src + row * KT::ROWB + tl.chunk_bytes(i) : (const char *)px_zero_row;
-                __builtin_amdgcn_global_load_lds((gptr_t)at, (lptr_t)(tile + i * WAVE), 16, 0, 0);
+                const char *at = (there >> r) & 1 ? src + row * KT::ROWB + tl.chunk_bytes(i) : (const char *)&px_zeros;
+                __builtin_amdgcn_global_load_lds((gptr_t)at, (lptr_t)(tile + i * WAVE), 16, 0, HINT);
             }
         }
     }

@@ -101,11 +101,11 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
     __shared__ u32x4 kt[KT::SLOTS], vt[KT::SLOTS];           // (two objects: see attn_lse_kernel)
     const int lane = threadIdx.x;
     // the tails first: their keys are found by way of lengths and page table, and they may be the longer ones
-    const int units_t = a.stream ? 0 : a.B * a.tiles_t * a.H * a.splits_t;
+    const int units_t = a.B * a.tiles_t * a.H * a.splits_t;
     int u = blockIdx.x;
     const bool tail = u < units_t;
     PageWindow win(a, 0);
-    int h, s, b = 0, p = -1, j0, end, least = 0;              // least: tokens that every query of the tile sees
+    int h, s, b = 0, p = -1, j0, end, total, least = 0;              // least: tokens that every query of the tile sees
     int64_t lin, lin_end;
     if (!tail) {
         u -= units_t;
@@ -130,6 +130,7 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
         const int n = prefix_len(a, p, h), part = part_keys(n, a.splits_p);
         j0 = s * part;
         end = min(n, j0 + part);
+        total = n;
     } else {
         s = u % a.splits_t;
         u /= a.splits_t;
@@ -147,9 +148,11 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
         const int t_first = (int)((lin - row_lin) / a.G), t_last = (int)((min(lin + PX_QUERIES, lin_end) - 1 - row_lin) / a.G);
         least = min(max(n - n_new + t_first + 1, 0), n);
         j0 = s * part;
+        total = n;
         end = min(min(max(n - n_new + t_last + 1, 0), n), j0 + part);
     }
     if (j0 >= end) return;
+    const bool stream = total >= (tail ? a.stream_t : a.stream_p);
 
     const TileLane<T> tl(lane);
     Queries<T> qs;
@@ -159,9 +162,12 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
         return rows.of_prefix(((size_t)p * a.H + h) * a.cap, j, end);
     };
     const char *K = (const char *)(tail ? a.Kt : a.Kp), *V = (const char *)(tail ? a.Vt : a.Vp);
+    const auto load = [&](const char *src, u32x4 *tile) {
+        if (stream) rows.template load<2>(tl, src, tile); else rows.template load<0>(tl, src, tile);
+    };
     uint32_t next = find(j0);
-    rows.load(tl, K, kt);
-    rows.load(tl, V, vt);
+    load(K, kt);
+    load(V, vt);
     qs.init(a, lin + (lane & 31), lin_end, h);
     int stop = end;                                          // tokens from here on one at a time
     for (int j = j0; j < end; j += 32) {
@@ -171,7 +177,7 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
         wait_lds();
         if (j + 32 < end) {
             next = find(j + 32);
-            rows.load(tl, K, kt);
+            load(K, kt);
             wait_vmcnt<KT::LOADS>();
         } else {
             wait_vmcnt<0>();
@@ -184,7 +190,7 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
         qs.weights(x, a.c);
         qs.values(tl, x, vt);
         wait_lds();
-        if (j + 32 < end) rows.load(tl, V, vt);
+        if (j + 32 < end) load(V, vt);
     }
     wait_vmcnt<0>();
     if (stop < end) one_by_one<T>(a, qs, b, h, stop, end);   // (tails only)
@@ -235,7 +241,7 @@ template <typename T> struct WideLoad {
             for (int i = 0; i < N; ++i) {
                 const uint32_t at = (32 * s + row[i]) * KT::ROWB + off[i];
                 const bool ok = j0 + 32 * s + row[i] < n;
-                const char *ks = ok ? kb + at : (const char *)px_zero_row, *vs = ok ? vb + at : (const char *)px_zero_row;
+                const char *ks = ok ? kb + at : (const char *)&px_zeros, *vs = ok ? vb + at : (const char *)&px_zeros;
                 __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(kt + s * KT::SLOTS + (slot + i) * WAVE), 16, 0, 0);
                 __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(vt + s * KT::SLOTS + (slot + i) * WAVE), 16, 0, 0);
             }
@@ -256,7 +262,7 @@ template <typename T> struct WideLoad {
                 const int r = 32 * s + row[i];
                 const uint64_t at = (((uint64_t)(uint32_t)__shfl((int)hi, r, WAVE) << 32) | (uint32_t)__shfl((int)lo, r, WAVE)) * KT::ROWB + off[i];
                 const bool ok = (there >> r) & 1;
-                const char *ks = ok ? (const char *)a.Kt + at : (const char *)px_zero_row, *vs = ok ? (const char *)a.Vt + at : (const char *)px_zero_row;
+                const char *ks = ok ? (const char *)a.Kt + at : (const char *)&px_zeros, *vs = ok ? (const char *)a.Vt + at : (const char *)&px_zeros;
                 __builtin_amdgcn_global_load_lds((gptr_t)ks, (lptr_t)(kt + s * KT::SLOTS + (slot + i) * WAVE), 16, 0, 0);
                 __builtin_amdgcn_global_load_lds((gptr_t)vs, (lptr_t)(vt + s * KT::SLOTS + (slot + i) * WAVE), 16, 0, 0);
             }
@@ -377,235 +383,6 @@ __global__ __launch_bounds__(4 * WAVE, 2) void prefix_attn_wide_kernel(PrefixAtt
     store_part(a, qs, (size_t)qs.row * (splits + a.splits_t) + part, l);
 }
 
-// ---- a few queries -------------------------------------------------------------------------------
-
-// Up to NQ queries of one row (its T * G) over a part of its tail, or of its prefix, by a workgroup: rows go straight from memory into
-// registers, sixteen lanes a row, and the matrix cores have nothing to offer.  What bounds it: the read of the keys and values.  A lane
-// keeps KEYS keys and values on their way, the next keys while values are added up, the next values while scores are taken.
-//   a.splits_t tail parts a row, then, with PX_STREAM_ALL, a.splits_p parts of its prefix (a prefix that several rows share is
-//   better read by the kernels above, once for all).
-// A tail in one part whose prefix parts an earlier launch has left is joined with them here (PX_STREAM_JOIN).
-template <typename T, int NQ>
-struct StreamState {
-    float m[NQ], l[NQ], acc[NQ][8];
-};
-
-// an operation over the four 16-lane rows of a wave, every lane gets the result
-template <typename F> __device__ __forceinline__ float rows4_all(float v, F op) {
-    const uint32_t x = __builtin_bit_cast(uint32_t, v);
-    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    const uint32_t r0 = r[0], r1 = r[1];
-    const uint32_t y = __builtin_bit_cast(uint32_t, op(__builtin_bit_cast(float, r0), __builtin_bit_cast(float, r1)));
-    const auto t = __builtin_amdgcn_permlane32_swap(y, y, false, false);
-    const uint32_t t0 = t[0], t1 = t[1];
-    return op(__builtin_bit_cast(float, t0), __builtin_bit_cast(float, t1));
-}
-
-template <typename T, int NQ>
-__global__ __launch_bounds__(4 * WAVE, NQ <= 2 ? 3 : 2) void prefix_attn_stream_kernel(PrefixAttnArgs a)
-{
-    typedef typename Elem<T>::Raw Raw;
-    constexpr int WAVES = 4, KEYS = (NQ == 8 ? 4 : 8) / (sizeof(T) / 2), STEP = 4 * KEYS, ROUND = WAVES * STEP;   // keys of a lane, a wave, the workgroup
-    __shared__ float acc_of[WAVES][NQ][HEAD_DIM], m_of[WAVES][NQ], l_of[WAVES][NQ];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane16 = lane & 15, sub = lane >> 4;
-    const int units_t = a.B * a.H * a.splits_t;
-    int u = blockIdx.x;
-    const bool tail = u < units_t;
-    const int splits = tail ? a.splits_t : a.splits_p;
-    if (!tail) u -= units_t;
-    const int s = u % splits;
-    u /= splits;
-    const int h = u % a.H, b = u / a.H;
-    PageWindow win(a, b);
-    if (tail) win.load(0);                                    // (on its way with the lengths)
-    const int n_new = clamp_len(a.new_lens, b, a.T), n_tail = tail_len(a, b);
-    const int nq = n_new * a.G;
-    if (nq == 0) return;
-    const int p = tail && a.stream != PX_STREAM_JOIN ? -1 : prefix_of(a, b);
-    const int n = tail ? n_tail : prefix_len(a, p, h), part = part_keys(n, splits);
-    const int j0 = s * part, end = min(n, j0 + part);
-    if (j0 >= end && !(tail && a.stream == PX_STREAM_JOIN)) return;
-
-    const int64_t token0 = (int64_t)b * a.T;
-    Raw q[NQ];
-    int sees[NQ];
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-        const int t = min(i, nq - 1) / a.G, g = min(i, nq - 1) - t * a.G;
-        q[i] = Elem<T>::load((const T *)a.q + (token0 + t) * a.q_stride + (int64_t)(h * a.G + g) * HEAD_DIM, lane16);
-        sees[i] = tail ? min(max(n_tail - n_new + t + 1, 0), n_tail) : n;
-    }
-    const int least = sees[0];
-    StreamState<T, NQ> st;
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-        st.m[i] = PX_NONE;
-        st.l[i] = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) st.acc[i][e] = 0.f;
-    }
-    const size_t prefix_row = ((size_t)max(p, 0) * a.H + h) * a.cap;
-    // keys j + 4 i + sub of the wave: their rows, in elements of the pool or the prefix; negative where there is none
-    const auto row_of = [&](int j, int i) -> int64_t {
-        const int k = j + 4 * i + sub;
-        if (!tail) return k < end ? (int64_t)(prefix_row + k) : -1;
-        const int at = min(k, end - 1), page = win.page(at >> a.page_shift);
-        return k < end && page >= 0 ? (((int64_t)page * a.H + h) << a.page_shift) + (at & ((1 << a.page_shift) - 1)) : -1;
-    };
-    const char *Kb = (const char *)(tail ? a.Kt : a.Kp), *Vb = (const char *)(tail ? a.Vt : a.Vp);
-    constexpr int ROWB = HEAD_DIM * (int)sizeof(T);
-    const uint32_t in_four = sub * ROWB;                      // (four neighbouring rows a load: of one page, where pages have four tokens)
-    Raw kr[KEYS], vr[KEYS];
-    // keys or values [j, j + STEP) of the wave; returns which of this lane's are there
-    const auto load = [&](const char *base, int j, Raw *r) -> uint32_t {
-        uint32_t there = 0;
-        if (j + STEP <= end && (!tail || a.page_shift >= 2)) {
-#pragma unroll
-            for (int i = 0; i < KEYS; ++i) {
-                const char *four = base + (prefix_row + j + 4 * i) * ROWB;
-                bool ok = true;
-                if (tail) {
-                    const int page = win.page_uniform((j + 4 * i) >> a.page_shift);
-                    ok = page >= 0;
-                    four = ok ? base + (size_t)((((int64_t)page * a.H + h) << a.page_shift) + ((j + 4 * i) & ((1 << a.page_shift) - 1))) * ROWB
-                              : (const char *)px_zero_row;
-                }
-                r[i] = Elem<T>::load_stream((const T *)(four + in_four), lane16);
-                there |= (uint32_t)ok << i;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < KEYS; ++i) {
-                const int64_t row = row_of(j, i);
-                r[i] = Elem<T>::load_stream((const T *)(row >= 0 ? base + row * ROWB : (const char *)px_zero_row), lane16);
-                there |= (uint32_t)(row >= 0) << i;
-            }
-        }
-        return there;
-    };
-    const auto need = [&](int j) { if (tail) win.need(j >> a.page_shift, (min(j + STEP, end) - 1) >> a.page_shift); };
-    uint32_t there = 0;
-    int j = j0 + wave * STEP;
-    if (j < end) {
-        need(j);
-        there = load(Kb, j, kr);
-        load(Vb, j, vr);
-    }
-    for (; j < end; j += ROUND) {
-        float x[NQ][KEYS];
-#pragma unroll
-        for (int i = 0; i < KEYS; ++i)
-#pragma unroll
-            for (int k = 0; k < NQ; ++k) x[k][i] = row16_sum(RowDot<T>::dot(kr[i], q[k])) * a.c;
-        const bool more = j + ROUND < end;
-        const bool mixed = a.T > 1 && tail && j + STEP > least;
-#pragma unroll
-        for (int i = 0; i < KEYS; ++i)
-#pragma unroll
-            for (int k = 0; k < NQ; ++k)
-                if (!((there >> i) & 1) || (mixed && j + 4 * i + sub >= sees[k])) x[k][i] = -INFINITY;
-        if (more) {
-            need(j + ROUND);
-            there = load(Kb, j + ROUND, kr);
-        }
-#pragma unroll
-        for (int k = 0; k < NQ; ++k) {
-            float top = x[k][0];
-#pragma unroll
-            for (int i = 1; i < KEYS; ++i) top = fmaxf(top, x[k][i]);
-            top = fmaxf(top, st.m[k]);
-            const float scale = __builtin_amdgcn_exp2f(st.m[k] - top);
-            st.m[k] = top;
-            st.l[k] *= scale;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) st.acc[k][e] *= scale;
-#pragma unroll
-            for (int i = 0; i < KEYS; ++i) {
-                x[k][i] = __builtin_amdgcn_exp2f(x[k][i] - top);
-                st.l[k] += x[k][i];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < KEYS; ++i) {
-            float v[8];
-            Elem<T>::to_float(vr[i], v);
-#pragma unroll
-            for (int k = 0; k < NQ; ++k) {
-                if (mixed) {                                  // (a value that the query does not see may be infinite)
-                    const bool seen = j + 4 * i + sub < sees[k];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) st.acc[k][e] = seen ? fmaf(x[k][i], v[e], st.acc[k][e]) : st.acc[k][e];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) st.acc[k][e] = fmaf(x[k][i], v[e], st.acc[k][e]);
-                }
-            }
-        }
-        if (more) load(Vb, j + ROUND, vr);
-    }
-    // the four rows of the wave, then the four waves
-#pragma unroll
-    for (int k = 0; k < NQ; ++k) {
-        const float top = rows4_all(st.m[k], [](float x, float y) { return fmaxf(x, y); });
-        const float scale = __builtin_amdgcn_exp2f(st.m[k] - top), l = rows4_sum(st.l[k] * scale);
-        float y[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = rows4_sum(st.acc[k][e] * scale);
-        if (sub == 0) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) acc_of[wave][k][lane16 * 8 + e] = y[e];
-        }
-        if (lane == 0) { m_of[wave][k] = top; l_of[wave][k] = l; }
-    }
-    __syncthreads();
-    // 32 lanes a query, four dimensions each; where prefix parts are joined, as many such groups a query as there are for them
-    const int lane32 = threadIdx.x & 31, slot = threadIdx.x >> 5;
-    constexpr int PER = 2 * WAVES / NQ;                       // groups a query
-    const int k = slot / PER, r = slot % PER;
-    const int t = k / a.G, g = k - t * a.G;
-    const int64_t row = (token0 + t) * (a.H * a.G) + h * a.G + g;
-    const size_t first = (size_t)row * (a.splits_p + a.splits_t);
-    const bool join = tail && a.stream == PX_STREAM_JOIN;
-    float top = PX_NONE, total = 0.f;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    const auto add = [&](float m, float l, const f32x4 &v) {
-        const float next = fmaxf(top, m), before = __builtin_amdgcn_exp2f(top - next), scale = __builtin_amdgcn_exp2f(m - next);
-        total = total * before + l * scale;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] = sum[e] * before + v[e] * scale;
-        top = next;
-    };
-    if (k < nq && join) {
-        const int used = parts_of_prefix(a, prefix_len(a, p, h));
-#pragma unroll 4
-        for (int i = r; i < used; i += PER)
-            add(a.stat[2 * (first + i)], a.stat[2 * (first + i) + 1], *reinterpret_cast<const f32x4 *>(a.part + (first + i) * HEAD_DIM + lane32 * 4));
-    }
-    if (k < nq && r == 0) {
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) add(m_of[w][k], l_of[w][k], *reinterpret_cast<const f32x4 *>(&acc_of[w][k][lane32 * 4]));
-    }
-    if (join && PER > 1) {
-        __shared__ f32x4 sum_of[2 * WAVES][32];
-        __shared__ float top_of[2 * WAVES], total_of[2 * WAVES];
-        sum_of[slot][lane32] = sum;
-        if (lane32 == 0) { top_of[slot] = top; total_of[slot] = total; }
-        __syncthreads();
-        if (r == 0) {
-#pragma unroll
-            for (int i = 1; i < PER; ++i) add(top_of[slot + i], total_of[slot + i], sum_of[slot + i][lane32]);
-        }
-    }
-    if (k >= nq || r != 0) return;
-    if (join) {
-        store_out<T>(a, row, lane32, top, total, sum);
-    } else {
-        const size_t at = first + (tail ? a.splits_p + s : s);
-        *reinterpret_cast<f32x4 *>(a.part + at * HEAD_DIM + lane32 * 4) = sum;
-        if (lane32 == 0) { a.stat[2 * at] = top; a.stat[2 * at + 1] = total; }
-    }
-}
-
 // ---- joining ---------------------------------------------------------------------------------------
 
 // The parts of a query: GROUPS groups of 32 lanes a query row, four dimensions a lane, the parts dealt to the groups.  Bound by the way of
@@ -706,12 +483,12 @@ __global__ __launch_bounds__(PX_JOIN_ROWS * 32) void prefix_attn_join_kernel(Pre
 
 // ---- host side ------------------------------------------------------------------------------------
 
-// Parts of a list of keys that is `most` long at most, `units` of them at a time: as many as fill the chip's `slots` once, of `least` keys each
-// at least; where there is more to read, four times as many, of 512 each, so that the last ones to end leave little of the chip idle.
-static int parts_for(int64_t units, int64_t most, int64_t slots, int64_t least)
+// Parts of a list of keys that is `most` long at most, `units` of them at a time: as many as make `waves` of them, of 64 keys each at least;
+// where there is more to read, four times as many, of 512 each, so that the last ones to end leave little of the chip idle.
+static int parts_for(int64_t units, int64_t most, int64_t waves)
 {
     if (units <= 0 || most <= 0) return 0;
-    const int64_t one_round = std::min<int64_t>(slots / units, most / least), rounds = std::min<int64_t>(4 * slots / units, most / 512);
+    const int64_t one_round = std::min<int64_t>(waves / units, most / 64), rounds = std::min<int64_t>(4 * waves / units, most / 512);
     return (int)std::max<int64_t>(1, std::max(one_round, rounds));
 }
 
@@ -719,6 +496,14 @@ static int tiles_of_prompts(const PrefixAttnArgs &a, int queries)
 {
     const int64_t per_row = (int64_t)a.T * a.G;
     return (int)(a.row_start ? a.B * per_row / queries + a.P : a.P * (((int64_t)(a.B / a.P) * per_row + queries - 1) / queries));
+}
+
+// Keys and values that one wave reads carry the non-temporal hint where `rows` lists as long as theirs come to half the last-level cache: by
+// a list's own length, as lengths are on the device.
+static int stream_keys(int64_t rows, const kvm_shape &sh)
+{
+    const int64_t per_key = rows * sh.H_kv * 2 * HEAD_DIM * (sh.dtype == KVM_F32 ? 4 : 2);
+    return (int)std::min<int64_t>((LLC_BYTES / 2 + per_key - 1) / per_key, INT32_MAX);
 }
 
 static void plan(const kvm_shape &sh, const kvm_prefix *prefix, const kvm_pages *pages, PrefixAttnArgs &a)
@@ -742,33 +527,27 @@ static void plan(const kvm_shape &sh, const kvm_prefix *prefix, const kvm_pages 
             a.splits_p = (int)std::max<int64_t>(1, std::min<int64_t>(512 / wide_rows, (a.cap + tail_most) / 256));
             return;
         }
-        if (a.P && (a.B / a.P) * per_row >= PX_WIDE) {
+        if (a.P && (a.B / a.P) * per_row >= 4 * PX_WIDE) {
             a.wide = PX_WIDE_PREFIX;
             a.tiles_p = tiles_of_prompts(a, PX_WIDE);
-            a.splits_p = (int)std::max<int64_t>(1, std::min<int64_t>(512 / wide_prompts, a.cap / 256));
+            a.splits_p = (int)std::max<int64_t>(1, std::min<int64_t>(256 / wide_prompts, a.cap / 256));
         }
     }
-    a.stream = per_row <= 8 && a.table ? (a.P && a.B > a.P ? PX_STREAM_TAILS : PX_STREAM_ALL) : PX_STREAM_NONE;
-    if (per_row <= 8 && a.P && a.B <= a.P) a.stream = PX_STREAM_ALL;
-    if (a.stream == PX_STREAM_ALL) {
-        // a row's prefix and tail are worked on at the same time: both of them fill the chip
-        a.splits_p = a.P ? parts_for((int64_t)a.B * a.H, a.cap, 512, 128) : 0;
-        a.splits_t = a.table ? parts_for((int64_t)a.B * a.H, tail_most, 512, 128) : 0;
-        a.wide = PX_WIDE_NONE;
-        if (a.splits_p == 0 && a.splits_t == 1) a.stream = PX_STREAM_JOIN;   // nothing to join: it writes the output itself
-        return;
+    // A compute unit holds eight waves of the split kernel.  The tails get parts for all of them, the prefixes for what the tails leave, a
+    // quarter at least: their parts are joined for every one of their rows.
+    int64_t units_t = 0;
+    if (a.table) {
+        a.tiles_t = (int)((per_row + PX_QUERIES - 1) / PX_QUERIES);
+        a.splits_t = parts_for((int64_t)a.B * a.tiles_t * a.H, tail_most, 2048);
+        units_t = (int64_t)a.B * a.tiles_t * a.H * a.splits_t;
     }
     if (a.P && !a.wide) {
+        const int64_t units = std::max<int64_t>((a.B * per_row + PX_QUERIES - 1) / PX_QUERIES, a.P) * a.H;
         a.tiles_p = tiles_of_prompts(a, PX_QUERIES);
-        a.splits_p = parts_for((a.B * per_row + PX_QUERIES - 1) / PX_QUERIES * a.H, a.cap, 1024, 64);
+        a.splits_p = parts_for(units, a.cap, std::max<int64_t>(512, std::min<int64_t>(2048 - units_t, 1024)));
+        a.stream_p = a.B * per_row <= (int64_t)a.P * PX_QUERIES ? stream_keys(a.P, sh) : INT32_MAX;
     }
-    if (a.stream) {
-        a.splits_t = parts_for((int64_t)a.B * a.H, tail_most, 512, 128);
-        if (a.splits_t == 1) a.stream = PX_STREAM_JOIN;
-    } else if (a.table) {
-        a.tiles_t = (int)((per_row + PX_QUERIES - 1) / PX_QUERIES);
-        a.splits_t = parts_for((int64_t)a.B * a.tiles_t * a.H, tail_most, 1024, 64);
-    }
+    a.stream_t = a.tiles_t == 1 ? stream_keys(a.B, sh) : INT32_MAX;
 }
 
 static int64_t query_rows(const PrefixAttnArgs &a) { return (int64_t)a.B * a.T * a.H * a.G; }
@@ -796,26 +575,13 @@ static kvm_status launch_t(const PrefixAttnArgs &a, hipStream_t st)
         }
     }
     int64_t units = 0;
-    if (!a.wide && a.stream != PX_STREAM_ALL) units += (int64_t)a.tiles_p * a.H * a.splits_p;
-    if (a.wide != PX_WIDE_ROWS && !a.stream) units += (int64_t)a.B * a.tiles_t * a.H * a.splits_t;
+    if (!a.wide) units += (int64_t)a.tiles_p * a.H * a.splits_p;
+    if (a.wide != PX_WIDE_ROWS) units += (int64_t)a.B * a.tiles_t * a.H * a.splits_t;
     if (units > 0) {
         ProfScope prof("prefix_attn_split_kernel", st);
         hipLaunchKernelGGL(prefix_attn_split_kernel<T>, dim3((unsigned)units), dim3(WAVE), 0, st, a);
         rc = check_launch("prefix_attn_split_kernel");
         if (rc != KVM_OK) return rc;
-    }
-    if (a.stream) {
-        const int64_t blocks = (int64_t)a.B * a.H * (a.splits_t + (a.stream == PX_STREAM_ALL ? a.splits_p : 0));
-        const auto stream = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(4 * WAVE), 0, st, a); };
-        ProfScope prof("prefix_attn_stream_kernel", st);
-        switch (a.T * a.G) {
-        case 1: stream(prefix_attn_stream_kernel<T, 1>); break;
-        case 2: stream(prefix_attn_stream_kernel<T, 2>); break;
-        case 3: case 4: stream(prefix_attn_stream_kernel<T, 4>); break;
-        default: stream(prefix_attn_stream_kernel<T, 8>);
-        }
-        rc = check_launch("prefix_attn_stream_kernel");
-        if (rc != KVM_OK || a.stream == PX_STREAM_JOIN) return rc;
     }
     ProfScope prof("prefix_attn_join_kernel", st);
     const auto join = [&](auto kernel, int groups) {
