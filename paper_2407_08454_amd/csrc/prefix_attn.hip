@@ -94,18 +94,16 @@ __device__ __forceinline__ int parts_of_prefix(const PrefixAttnArgs &a, int n) {
 // What bounds it: the read of the keys and values.  A wave has room for one tile of 32 keys and one of their values in LDS: the next keys are
 // asked for as soon as the scores are taken, the next values when they have been added up, so that one of the two is always on its way
 // and mostly both.  Nobody waits for anybody.
+//   u: tail parts first (their keys are found by way of lengths and page table, and they may be the longer ones), then prefix parts.
 template <typename T>
-__global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_split_kernel(PrefixAttnArgs a)
+__device__ __forceinline__ void split_unit(const PrefixAttnArgs &a, int u, u32x4 *kt, u32x4 *vt)
 {
     using KT = KeyTile<T>;
-    __shared__ u32x4 kt[KT::SLOTS], vt[KT::SLOTS];           // (two objects: see attn_lse_kernel)
-    const int lane = threadIdx.x;
-    // the tails first: their keys are found by way of lengths and page table, and they may be the longer ones
+    const int lane = threadIdx.x & 63;
     const int units_t = a.B * a.tiles_t * a.H * a.splits_t;
-    int u = blockIdx.x;
     const bool tail = u < units_t;
     PageWindow win(a, 0);
-    int h, s, b = 0, p = -1, j0, end, total, least = 0;              // least: tokens that every query of the tile sees
+    int h, s, b = 0, p = -1, j0, end, total, least = 0;       // least: tokens that every query of the tile sees
     int64_t lin, lin_end;
     if (!tail) {
         u -= units_t;
@@ -114,7 +112,7 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
         int group, tile;
         if (groups % 8 == 0) {
             const int slot = u >> 3;
-            group = slot / a.tiles_p * 8 + (blockIdx.x & 7);
+            group = slot / a.tiles_p * 8 + (u & 7);
             tile = slot % a.tiles_p;
         } else {
             group = u / a.tiles_p;
@@ -200,11 +198,18 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
     store_part(a, qs, (size_t)qs.row * (a.splits_p + a.splits_t) + (tail ? a.splits_p + s : s), l);
 }
 
+template <typename T>
+__global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_split_kernel(PrefixAttnArgs a)
+{
+    __shared__ u32x4 kt[KeyTile<T>::SLOTS], vt[KeyTile<T>::SLOTS];   // (two objects: see attn_lse_kernel)
+    split_unit<T>(a, blockIdx.x, kt, vt);
+}
+
 // The same for many queries: a workgroup of four waves has 128 of them and takes 64 keys at a time, which its waves load together and share.
 // What bounds it: the matrix cores, with the exponentials beside them, and the fragments' way out of LDS (a fragment serves 32 queries).
 // Two workgroups on a compute unit work on their exponentials in turn.
 //   ROWS: the queries of one row and all their keys, prefix and tail one after the other in tiles of 64, in one part or several;
-//   else: the queries of a prompt's rows and a part of their prefix.
+//   else: the queries of a prompt's rows and a part of their prefix; the last workgroups have tail parts as above, one a wave.
 constexpr int PX_WIDE = 128;
 
 // A wave's share of a tile of 64 keys: rows r[0], r[1] of each half.
@@ -275,17 +280,25 @@ __global__ __launch_bounds__(4 * WAVE, 2) void prefix_attn_wide_kernel(PrefixAtt
 {
     using KT = KeyTile<T>;
     __shared__ u32x4 k_a[2 * KT::SLOTS], v_a[2 * KT::SLOTS], k_b[2 * KT::SLOTS], v_b[2 * KT::SLOTS];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int block = blockIdx.x;
+    if (!ROWS && block >= a.tiles_p * a.H * a.splits_p) {
+        const int u = __builtin_amdgcn_readfirstlane(4 * (block - a.tiles_p * a.H * a.splits_p) + wave), at = (wave & 1) * KT::SLOTS;
+        if (u >= a.B * a.tiles_t * a.H * a.splits_t) return;
+        if (wave < 2) split_unit<T>(a, u, k_a + at, v_a + at);
+        else split_unit<T>(a, u, k_b + at, v_b + at);
+        return;
+    }
     const int tiles = ROWS ? a.B * a.tiles_t : a.tiles_p, splits = a.splits_p;
     const int groups = a.H * splits;
     int group, tile;
     if (groups % 8 == 0) {
-        const int slot = blockIdx.x >> 3;
-        group = slot / tiles * 8 + (blockIdx.x & 7);
+        const int slot = block >> 3;
+        group = slot / tiles * 8 + (block & 7);
         tile = slot % tiles;
     } else {
-        group = blockIdx.x / tiles;
-        tile = blockIdx.x % tiles;
+        group = block / tiles;
+        tile = block % tiles;
     }
     const int h = group % a.H, part = group / a.H;
     int b = 0, p, n_tail = 0, n_new = 0;
@@ -527,7 +540,9 @@ static void plan(const kvm_shape &sh, const kvm_prefix *prefix, const kvm_pages 
             a.splits_p = (int)std::max<int64_t>(1, std::min<int64_t>(512 / wide_rows, (a.cap + tail_most) / 256));
             return;
         }
-        if (a.P && (a.B / a.P) * per_row >= 4 * PX_WIDE) {
+        // bf16, 8 KV heads, 6500 states, 64 tokens a tail, us both launches, by 32 / by 128 queries: 128 queries of a prompt share them 25.8 / 22.8,
+        // 256 35.7 / 28.4, 1024 79 / 57
+        if (a.P && a.B * per_row >= (int64_t)a.P * PX_WIDE) {
             a.wide = PX_WIDE_PREFIX;
             a.tiles_p = tiles_of_prompts(a, PX_WIDE);
             a.splits_p = (int)std::max<int64_t>(1, std::min<int64_t>(256 / wide_prompts, a.cap / 256));
@@ -566,7 +581,9 @@ static kvm_status launch_t(const PrefixAttnArgs &a, hipStream_t st)
     kvm_status rc = KVM_OK;
     if constexpr (sizeof(T) == 2) {
         if (a.wide) {
-            const int64_t blocks = (int64_t)(a.wide == PX_WIDE_ROWS ? a.B * a.tiles_t : a.tiles_p) * a.H * a.splits_p;
+            const int64_t units_t = (int64_t)a.B * a.tiles_t * a.H * a.splits_t;
+            const int64_t blocks = a.wide == PX_WIDE_ROWS ? (int64_t)a.B * a.tiles_t * a.H * a.splits_p
+                                                          : (int64_t)a.tiles_p * a.H * a.splits_p + (units_t + 3) / 4;
             ProfScope prof("prefix_attn_wide_kernel", st);
             if (a.wide == PX_WIDE_ROWS) hipLaunchKernelGGL((prefix_attn_wide_kernel<T, true>), dim3((unsigned)blocks), dim3(4 * WAVE), 0, st, a);
             else hipLaunchKernelGGL((prefix_attn_wide_kernel<T, false>), dim3((unsigned)blocks), dim3(4 * WAVE), 0, st, a);
@@ -574,9 +591,7 @@ static kvm_status launch_t(const PrefixAttnArgs &a, hipStream_t st)
             if (rc != KVM_OK || direct(a)) return rc;
         }
     }
-    int64_t units = 0;
-    if (!a.wide) units += (int64_t)a.tiles_p * a.H * a.splits_p;
-    if (a.wide != PX_WIDE_ROWS) units += (int64_t)a.B * a.tiles_t * a.H * a.splits_t;
+    const int64_t units = a.wide ? 0 : (int64_t)a.tiles_p * a.H * a.splits_p + (int64_t)a.B * a.tiles_t * a.H * a.splits_t;
     if (units > 0) {
         ProfScope prof("prefix_attn_split_kernel", st);
         hipLaunchKernelGGL(prefix_attn_split_kernel<T>, dim3((unsigned)units), dim3(WAVE), 0, st, a);
