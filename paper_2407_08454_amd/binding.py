@@ -381,6 +381,7 @@ def make_pages(K_pages: torch.Tensor, V_pages: torch.Tensor, table: torch.Tensor
     n_pages, _, page_size, _ = K_pages.shape
     pages = KvmPages(K_pages.data_ptr(), V_pages.data_ptr(), table.data_ptr(), n_pages, page_size, table.shape[1])
     pages._refs = (K_pages, V_pages, table)   # the descriptor holds raw pointers: keep the tensors alive
+    pages._fits = (K_pages.shape[1], K_pages.shape[3], _TORCH_DTYPE[K_pages.dtype], K_pages.get_device(), table.shape[0])
     return pages
 
 
@@ -412,6 +413,7 @@ def make_prefix(K: torch.Tensor, V: torch.Tensor, lens: torch.Tensor | None = No
         raise ValueError("row_start must be int32 of shape (P + 1,)")
     prefix = KvmPrefix(K.data_ptr(), V.data_ptr(), _ptr(lens), _ptr(row_start), P, cap)
     prefix._refs = (K, V, lens, row_start)
+    prefix._fits = (H, K.shape[3], _TORCH_DTYPE[K.dtype], K.get_device(), None)
     return prefix
 
 
@@ -433,66 +435,74 @@ def make_token_shape(cache: KvmPages | KvmPrefix, T: int, G: int = 1, new_lens: 
     return shape
 
 
+_DTYPE = {code: dtype for dtype, code in _TORCH_DTYPE.items()}
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _current_stream():
+    """The current device, and the handle of its current stream."""
+    current = _get_device()
+    return current, torch.cuda.current_stream().cuda_stream if _current_raw_stream is None else _current_raw_stream(current)
+
+
 def _check_cache(shape, cache, current):
     """A cache descriptor fits the shape and lives on the current device, whose stream the call goes to."""
-    K = cache._refs[0]
-    if K.get_device() != current:
+    H, d, dtype, device, rows = cache._fits
+    if device != current:
         raise ValueError("the cache is not on the current device")
-    if K.shape[1] != shape.H_kv or K.shape[3] != shape.d or _TORCH_DTYPE[K.dtype] != shape.dtype:
+    if H != shape.H_kv or d != shape.d or dtype != shape.dtype:
         raise ValueError("the cache does not match the shape descriptor")
-    if isinstance(cache, KvmPages) and cache._refs[2].shape[0] != shape.B:
+    if rows is not None and rows != shape.B:
         raise ValueError("the page table does not match the shape descriptor")
 
 
-def _token_stride(name, t, B, T, heads, d, dtype, current):
+def _token_stride(name, t, want, dtype, current):
     """Elements between consecutive tokens of a (B, T, heads, d) tensor or view whose heads are contiguous."""
-    if t.shape != (B, T, heads, d) or _TORCH_DTYPE.get(t.dtype) != dtype:
-        raise ValueError(f"{name} has shape {tuple(t.shape)} and dtype {t.dtype}, expected {(B, T, heads, d)} of the cache's dtype")
+    if t.shape != want or t.dtype != dtype:
+        raise ValueError(f"{name} has shape {tuple(t.shape)} and dtype {t.dtype}, expected {want} and {dtype}")
     if t.get_device() != current:
         raise ValueError(f"{name} is not on the current GPU")
+    B, T, heads, d = want
     row, token, head, elem = t.stride()
     if T == 1:
-        token = row
-    if B == 1 and T == 1:
-        token = heads * d
+        token = row if B > 1 else heads * d
     if elem != 1 or (head != d and heads > 1) or (B > 1 and row != T * token):
         raise ValueError(f"{name}: the heads of a token must be contiguous and the tokens evenly spaced")
     return token
 
 
-def _lens_vector(name, t, B, current):
-    if t.dtype != torch.int32 or t.shape != (B,) or not t.is_contiguous() or t.get_device() != current:
-        raise ValueError(f"{name} must be a contiguous int32 tensor of shape (B,) on the current GPU")
+def _check_out(name, t, want, dtype, current):
+    if t is None or t.shape != want or t.dtype != dtype or t.get_device() != current or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {want} on the current GPU")
 
 
 def kvm_paged_append(shape: KvmShape, pages: KvmPages, rotation: KvmRotation, q_new, k_new, v_new, past_lens, pos_base, q_out,
                      kv_lens):
     """The step's keys (rotated) and values into the rows' pages, rotated queries to q_out, kv_lens <- past_lens + new tokens."""
-    B, H, G, T, d = shape.B, shape.H_kv, shape.G, shape.N, shape.d
-    current = torch.cuda.current_device()
+    B, H, T, d, dtype = shape.B, shape.H_kv, shape.N, shape.d, _DTYPE.get(shape.dtype)
+    current, stream = _current_stream()
     _check_cache(shape, pages, current)
-    ks = _token_stride("k_new", k_new, B, T, H, d, shape.dtype, current)
-    vs = _token_stride("v_new", v_new, B, T, H, d, shape.dtype, current)
+    kv, lens = (B, T, H, d), (B,)
+    ks = _token_stride("k_new", k_new, kv, dtype, current)
+    vs = _token_stride("v_new", v_new, kv, dtype, current)
     qs = 0
     if q_new is not None:
-        qs = _token_stride("q_new", q_new, B, T, H * G, d, shape.dtype, current)
-        if q_out is None or not q_out.is_contiguous():
-            raise ValueError("q_out must be contiguous")
-        _token_stride("q_out", q_out, B, T, H * G, d, shape.dtype, current)
-    _lens_vector("past_lens", past_lens, B, current)
-    _lens_vector("kv_lens", kv_lens, B, current)
+        q = (B, T, H * shape.G, d)
+        qs = _token_stride("q_new", q_new, q, dtype, current)
+        _check_out("q_out", q_out, q, dtype, current)
+    _check_out("past_lens", past_lens, lens, torch.int32, current)
+    _check_out("kv_lens", kv_lens, lens, torch.int32, current)
     if pos_base is not None:
-        _lens_vector("pos_base", pos_base, B, current)
+        _check_out("pos_base", pos_base, lens, torch.int32, current)
     if rotation._ref is not None and rotation._ref.get_device() != current:
         raise ValueError("inv_freq is not on the current GPU")
     _check("kvm_paged_append", load_library().kvm_paged_append(
-        ctypes.byref(shape), ctypes.byref(pages), ctypes.byref(rotation), _ptr(q_new), qs, k_new.data_ptr(), ks, v_new.data_ptr(), vs,
-        past_lens.data_ptr(), _ptr(pos_base), _ptr(q_out), kv_lens.data_ptr(), _stream()))
+        shape, pages, rotation, _ptr(q_new), qs, k_new.data_ptr(), ks, v_new.data_ptr(), vs, past_lens.data_ptr(), _ptr(pos_base),
+        _ptr(q_out), kv_lens.data_ptr(), stream))
 
 
 def kvm_prefix_attn_workspace_bytes(shape: KvmShape, prefix: KvmPrefix | None, pages: KvmPages | None) -> int:
-    need = load_library().kvm_prefix_attn_workspace_bytes(ctypes.byref(shape), None if prefix is None else ctypes.byref(prefix),
-                                                          None if pages is None else ctypes.byref(pages))
+    need = load_library().kvm_prefix_attn_workspace_bytes(shape, prefix, pages)
     if need == 0:
         raise KvmError("kvm_prefix_attn_workspace_bytes", KVM_ERR_INVALID_ARG, load_library().kvm_last_error().decode())
     return need
@@ -500,24 +510,22 @@ def kvm_prefix_attn_workspace_bytes(shape: KvmShape, prefix: KvmPrefix | None, p
 
 def kvm_prefix_attn(shape: KvmShape, prefix: KvmPrefix | None, pages: KvmPages | None, Q, kv_lens, out, lse_opt, ws):
     """out (B, T, H_kv*G, d) <- attention of Q over the rows' shared prefixes and their own pages; lse_opt (B, T, H_kv*G) float32."""
-    B, H, G, T, d = shape.B, shape.H_kv, shape.G, shape.N, shape.d
-    current = torch.cuda.current_device()
-    for cache in (prefix, pages):
-        if cache is not None:
-            _check_cache(shape, cache, current)
-    qs = _token_stride("Q", Q, B, T, H * G, d, shape.dtype, current)
-    _token_stride("out", out, B, T, H * G, d, shape.dtype, current)
-    if not out.is_contiguous() or not ws.is_contiguous() or ws.get_device() != current:
-        raise ValueError("out and ws must be contiguous, ws on the current GPU")
+    rows, dtype = (shape.B, shape.N, shape.H_kv * shape.G, shape.d), _DTYPE.get(shape.dtype)
+    current, stream = _current_stream()
+    if prefix is not None:
+        _check_cache(shape, prefix, current)
     if pages is not None:
-        _lens_vector("kv_lens", kv_lens, B, current)
-    if lse_opt is not None and (lse_opt.dtype != torch.float32 or lse_opt.shape != (B, T, H * G) or not lse_opt.is_contiguous() or
-                                lse_opt.get_device() != current):
-        raise ValueError("lse_opt must be a contiguous float32 tensor of shape (B, T, H_kv*G) on the current GPU")
+        _check_cache(shape, pages, current)
+        _check_out("kv_lens", kv_lens, rows[:1], torch.int32, current)
+    qs = _token_stride("Q", Q, rows, dtype, current)
+    _check_out("out", out, rows, dtype, current)
+    if lse_opt is not None:
+        _check_out("lse_opt", lse_opt, rows[:3], torch.float32, current)
+    if not ws.is_contiguous() or ws.get_device() != current:
+        raise ValueError("ws must be contiguous and on the current GPU")
     _check("kvm_prefix_attn", load_library().kvm_prefix_attn(
-        ctypes.byref(shape), None if prefix is None else ctypes.byref(prefix), None if pages is None else ctypes.byref(pages),
-        Q.data_ptr(), qs, None if pages is None else kv_lens.data_ptr(), out.data_ptr(), _ptr(lse_opt), ws.data_ptr(),
-        ws.numel() * ws.element_size(), _stream()))
+        shape, prefix, pages, Q.data_ptr(), qs, None if pages is None else kv_lens.data_ptr(), out.data_ptr(), _ptr(lse_opt),
+        ws.data_ptr(), ws.nbytes, stream))
 
 
 def kvm_profile_enable(max_launches: int):

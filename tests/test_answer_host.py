@@ -157,7 +157,7 @@ def test_binding_refuses_tensors_that_are_not_on_the_gpu_or_do_not_fit():
     with pytest.raises(ValueError):
         kb.make_rotation(torch.zeros(64))
     # evenly spaced tokens whose heads are contiguous, nothing else
-    stride = lambda t, B, T, H: kb._token_stride("x", t, B, T, H, 128, kb.KVM_F32, t.get_device())
+    stride = lambda t, B, T, H: kb._token_stride("x", t, (B, T, H, 128), torch.float32, t.get_device())
     x = torch.zeros((2, 3, 6, 128))
     assert stride(x, 2, 3, 6) == 768 and stride(x[:, :, 2:4], 2, 3, 2) == 768 and stride(x[:, :1], 2, 1, 6) == 3 * 768
     assert stride(x[:1], 1, 3, 6) == 768 and stride(x[:1, 1:2], 1, 1, 6) == 768
