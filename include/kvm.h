@@ -394,7 +394,7 @@ kvm_status kvm_evict_merge_values(const kvm_shape *shape, const kvm_params *para
  * (NULL: all T); H_kv, G, d and dtype as elsewhere.  New tokens are token-major as a projection leaves them:
  * q (B, T, H_kv*G, d), k and v (B, T, H_kv, d), the heads of a token contiguous, consecutive tokens (also
  * of consecutive rows) *_stride elements apart, so that views of one fused projection need no copy.
- * Pointers and strides have to be multiples of 16 bytes.  A call takes up to 2^22 tokens (B * N) and 2^29 head rows
+ * Pointers and strides have to be multiples of 16 bytes.  A call takes up to 2^22 tokens (B * N) and 2^26 head rows
  * (B * N * H_kv * (G + 2)).
  */
 typedef struct {
@@ -462,8 +462,9 @@ kvm_status kvm_paged_append(const kvm_shape *shape, const kvm_pages *pages, cons
  *   out       out  (B, T, H_kv*G, d) contiguous; tokens t >= seq_lens[b] are left as they were
  *   lse_opt   out  (B, T, H_kv*G) float32 or NULL
  *   ws        kvm_prefix_attn_workspace_bytes(), 256-byte aligned; one call at a time
- * Scores, sums and outputs are accumulated in fp32; 16-bit types round the weights exp(score - running maximum)
- * once to dtype before they meet the values.  Deterministic: no atomics, and a call on the same shape repeats its
+ * Scores, sums and outputs are accumulated in fp32.  16-bit types: the weights exp(score - reference) meet the values as
+ * two numbers of dtype, the rounded weight and what the rounding left; where 128 queries are worked on at a time (128 of a row's,
+ * T * G, or on average of a prompt's) as the rounded one alone, half a step of a weight.  Deterministic: no atomics, and a call on the same shape repeats its
  * bits.  The order of the sums follows from the sizes in shape, prefix and pages and from the lengths, so a row in another batch
  * can differ in its last bits.
  */

@@ -203,7 +203,7 @@ static kvm_status check_prefix(const kvm_shape *sh, const kvm_prefix *px, const 
 static kvm_status check_tokens(const kvm_shape *sh, const char *fn)
 {
     const int64_t tokens = (int64_t)sh->B * sh->N;
-    if (tokens > (1ll << 22) || tokens * sh->H_kv * (sh->G + 2) > (1ll << 29)) {
+    if (tokens > (1ll << 22) || tokens * sh->H_kv * (sh->G + 2) > (1ll << 26)) {
         set_error("%s: %lld tokens with %d query and %d key heads are too many for one call", fn, (long long)tokens, sh->H_kv * sh->G, sh->H_kv);
         return KVM_ERR_UNSUPPORTED;
     }

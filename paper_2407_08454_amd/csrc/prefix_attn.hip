@@ -1,8 +1,13 @@
-// Attention of new tokens over the compacted cache of their prompt and over their row's own pages.
+// Attention of new tokens over the compacted cache of their prompt and over their row's own pages:
+//     out = sum_j w_j v_j,  w = softmax over all keys j that the query sees of q . k_j / sqrt(d).
+// One pass over the keys with a running reference and sum (prefix_attn.h), the keys split into parts where there are few queries, a part's
+// accumulators, reference and sum kept in fp32 in the workspace.
 //
 //   prefix_attn_split_kernel  32 queries and a part of their keys a wave.  The keys of a prefix are read once for 32 queries of
 //                             all the prompt's rows; a row's own tail for the queries of that row.
-//   prefix_attn_join_kernel   puts the parts of a query on one maximum and adds them up.
+//   prefix_attn_wide_kernel   128 queries a workgroup: many queries of one row, with all their keys, or the many rows of a prompt, with
+//                             a part of their prefix (16-bit types)
+//   prefix_attn_join_kernel   puts the parts of a query on one reference and adds them up
 #include <algorithm>
 
 #include "prefix_attn.h"
@@ -91,9 +96,11 @@ __device__ __forceinline__ int parts_of_prefix(const PrefixAttnArgs &a, int n) {
     return (n + part - 1) / part;
 }
 
-// What bounds it: the read of the keys and values.  A wave has room for one tile of 32 keys and one of their values in LDS: the next keys are
-// asked for as soon as the scores are taken, the next values when they have been added up, so that one of the two is always on its way
-// and mostly both.  Nobody waits for anybody.
+// What bounds it: the read of the keys and values (fp32: the matrix cores, 8192 cycles a tile of 32 keys).  A wave has room for one tile of 32
+// keys and one of their values in LDS: the next keys are asked for as soon as the scores are taken, the next values when they have been added
+// up, so that one of the two is always on its way and mostly both; eight waves of a compute unit keep 128 KB on their way (two stages a wave,
+// four waves: 37 rows over 2048 states and tails of up to 1000 tokens 88 us, this 72).  Nobody waits for anybody.  8 rows with tails of up to
+// 16384 tokens, 1.76 GB: 284 us, 6.2 TB/s.
 //   u: tail parts first (their keys are found by way of lengths and page table, and they may be the longer ones), then prefix parts.
 template <typename T>
 __device__ __forceinline__ void split_unit(const PrefixAttnArgs &a, int u, u32x4 *kt, u32x4 *vt)
@@ -186,7 +193,7 @@ __device__ __forceinline__ void split_unit(const PrefixAttnArgs &a, int u, u32x4
             if (mixed && a.T > 1 && has_nonfinite<T>(vt)) { stop = j; break; }
         }
         qs.weights(x, a.c);
-        qs.values(tl, x, vt);
+        qs.template values<true>(tl, x, vt);
         wait_lds();
         if (j + 32 < end) load(V, vt);
     }
@@ -206,8 +213,11 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
 }
 
 // The same for many queries: a workgroup of four waves has 128 of them and takes 64 keys at a time, which its waves load together and share.
-// What bounds it: the matrix cores, with the exponentials beside them, and the fragments' way out of LDS (a fragment serves 32 queries).
-// Two workgroups on a compute unit work on their exponentials in turn.
+// What bounds it: matrix cores (38 % busy), vector ALU (39 %, the exponentials) and the fragments' way out of LDS beside one another: two
+// workgroups a compute unit, two waves a SIMD, so one wave's exponentials meet the other's products by chance.  8 x 2048 tokens of 40 heads over
+// 5734 states and their own: 2.1 ms, 900 TFLOP/s, where a library product of 8192^3 reaches 1130.  Tried and slower: eight waves that change
+// over between products and exponentials at barriers (2.35 ms: their LDS reads fall together), 64 queries a wave with a SIMD to itself (2.88),
+// fragments read ahead (2.21), one half's exponentials written between the other's products (2.30).
 //   ROWS: the queries of one row and all their keys, prefix and tail one after the other in tiles of 64, in one part or several;
 //   else: the queries of a prompt's rows and a part of their prefix; the last workgroups have tail parts as above, one a wave.
 constexpr int PX_WIDE = 128;
@@ -356,8 +366,8 @@ __global__ __launch_bounds__(4 * WAVE, 2) void prefix_attn_wide_kernel(PrefixAtt
                 if (mixed && a.T > 1 && (has_nonfinite<T>(vt) || has_nonfinite<T>(vt + KT::SLOTS))) { stop = j; return; }
             }
             qs.weights(x0, x1, a.c);
-            qs.values(tl, x0, vt);
-            qs.values(tl, x1, vt + KT::SLOTS);
+            qs.template values<false>(tl, x0, vt);
+            qs.template values<false>(tl, x1, vt + KT::SLOTS);
         };
         uint64_t there_a = load(v, k_a, v_a), there_b = 0;
         for (;;) {
@@ -497,7 +507,8 @@ __global__ __launch_bounds__(PX_JOIN_ROWS * 32) void prefix_attn_join_kernel(Pre
 // ---- host side ------------------------------------------------------------------------------------
 
 // Parts of a list of keys that is `most` long at most, `units` of them at a time: as many as make `waves` of them, of 64 keys each at least;
-// where there is more to read, four times as many, of 512 each, so that the last ones to end leave little of the chip idle.
+// where there is more to read, four times as many, of 512 each, so that the last ones to end leave little of the chip idle.  (One row over 2048
+// states, us, parts of 64 / 96 keys 9.0 / 12.7; 8 rows with tails of up to 16384 tokens, 4 / 8 / 16 parts of a prefix 290 / 284 / 284.)
 static int parts_for(int64_t units, int64_t most, int64_t waves)
 {
     if (units <= 0 || most <= 0) return 0;
@@ -512,7 +523,8 @@ static int tiles_of_prompts(const PrefixAttnArgs &a, int queries)
 }
 
 // Keys and values that one wave reads carry the non-temporal hint where `rows` lists as long as theirs come to half the last-level cache: by
-// a list's own length, as lengths are on the device.
+// a list's own length, as lengths are on the device.  (37 rows, 436 MB, us, without / with 89 / 73; 32 rows, 211 MB that the last-level cache
+// still holds from the call before, 44 / 50.)
 static int stream_keys(int64_t rows, const kvm_shape &sh)
 {
     const int64_t per_key = rows * sh.H_kv * 2 * HEAD_DIM * (sh.dtype == KVM_F32 ? 4 : 2);
@@ -549,7 +561,8 @@ static void plan(const kvm_shape &sh, const kvm_prefix *prefix, const kvm_pages 
         }
     }
     // A compute unit holds eight waves of the split kernel.  The tails get parts for all of them, the prefixes for what the tails leave, a
-    // quarter at least: their parts are joined for every one of their rows.
+    // quarter at least: their parts are joined for every one of their rows.  (32 rows of two prompts, us, both launches, prefixes and tails in 16
+    // and 1 / 8 and 1 / 8 and 2 / 4 and 2 parts 57 / 52 / 44 / 47.)
     int64_t units_t = 0;
     if (a.table) {
         a.tiles_t = (int)((per_row + PX_QUERIES - 1) / PX_QUERIES);

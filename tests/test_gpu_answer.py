@@ -233,6 +233,8 @@ CASES = {
     "rows_31": dict(B=31, T=1, H=2, G=1, P=1, cap=77, kv=list(range(1, 32)), page=4),
     "rows_33": dict(B=33, T=1, H=2, G=1, P=1, cap=129, lens=[[129, 64]], kv=[5] * 33),
     "rows_130_g4": dict(B=130, T=1, H=1, G=4, P=1, cap=400, kv=[(7 * i) % 50 + 1 for i in range(130)]),
+    "many_rows_ragged": dict(B=150, T=2, H=2, G=1, P=2, cap=300, lens=[[300, 0], [129, 64]], row_start=[3, 100, 149], kv=[2 + (5 * i) % 70 for i in range(150)]),
+    "many_rows_prefix_alone": dict(B=140, T=1, H=1, G=2, P=2, cap=190, lens=[[190], [65]]),
     "g33": dict(B=3, T=1, H=1, G=33, P=1, cap=100, kv=[64, 65, 1]),
     # prompts with different numbers of rows, one without rows, rows of no prompt
     "ragged_prompts": dict(B=41, T=1, H=2, G=2, P=5, cap=200, lens=[[200, 3], [0, 150], [7, 7], [64, 65], [1, 0]], row_start=[1, 4, 4, 37, 39, 40],
@@ -268,6 +270,36 @@ CASES = {
 def test_attention(name, dtype):
     _say(f"attention {name} {dtype}")
     Attn(dtype, seed=11, **CASES[name]).run().check()
+
+
+@pytest.mark.parametrize("name,kernels", [
+    ("single_row", {"prefix_attn_split_kernel", "prefix_attn_join_kernel"}),
+    ("rows_33", {"prefix_attn_split_kernel", "prefix_attn_join_kernel"}),
+    ("rows_130_g4", {"prefix_attn_wide_kernel", "prefix_attn_join_kernel"}),           # 520 queries of a prompt
+    ("many_rows_ragged", {"prefix_attn_wide_kernel", "prefix_attn_join_kernel"}),
+    ("chunk_333", {"prefix_attn_wide_kernel", "prefix_attn_join_kernel"}),             # few tiles: their keys in parts
+    ("all_empty", {"prefix_attn_split_kernel", "prefix_attn_join_kernel"}),
+])
+def test_which_kernels_run(name, kernels):
+    a = Attn("bf16", seed=3, **CASES[name])
+    assert gu.kernels_of(a.call) == kernels
+
+
+def test_many_tokens_go_straight_to_the_output():
+    """Enough query tiles for the chip: prefix and tail in one pass, nothing to join."""
+    a = Attn("f16", B=9, T=100, H=8, G=10, seed=8, P=3, cap=70, lens=[[70] * 8, [1] * 8, [0] * 8], kv=[100 + i for i in range(9)], new=[100 - 11 * i for i in range(9)])
+    assert gu.kernels_of(a.call) == {"prefix_attn_wide_kernel"}
+    rows = [0, 4, 8]                                           # (the plain form of all of them takes long)
+    a.run()
+    for b in rows:
+        p = b // 3
+        out, lse, bounds = ar.attention(a.q64[b:b + 1], a.G, a.new[b:b + 1], dict(K=a.prefix64["K"][p:p + 1], V=a.prefix64["V"][p:p + 1],
+                                        lens=a.prefix64["lens"][p:p + 1], row_start=None), dict(a.pages64, table=a.pages64["table"][b:b + 1], kv_lens=a.pages64["kv_lens"][b:b + 1]))
+        o_tol, l_tol = ar.tolerance("f16", out, lse, bounds)
+        there = ~np.isnan(lse)
+        out[~there], lse[~there], o_tol[~there], l_tol[~there] = MARK, MARK, 0.0, 0.0
+        _check(a.lse[b:b + 1], lse, l_tol, f"lse of row {b}")
+        _check(a.out[b:b + 1], out, o_tol, f"out of row {b}")
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
