@@ -8,7 +8,7 @@
 // that turn together: chunks u and u + rot/16 where dimensions i and i + rot/2 pair up, neighbouring chunks where 2i and
 // 2i + 1 do; either way lane u of a row needs angles 8u .. 8u+7, the same for all rows of the token.  The wave's 64 lanes therefore
 // work out one angle each, while the rows are on their way, and exchange them through LDS.  16384 tokens of 40 heads in fp16, 1.0 GB read and
-// written: 176-190 us, 5.3-5.7 TB/s (a copy of 1 GiB runs at 5.2); one token 2.9 us, a launch.
+// written: 172 us, 5.9 TB/s (a copy of 1 GiB runs at 5.2); one token 2.9 us, a launch.
 #include "kvm_common.h"
 
 namespace kvm {
@@ -36,7 +36,7 @@ __device__ __forceinline__ float2 unit_at(int64_t x, float f) {
     return make_float2(c, s);
 }
 
-template <typename T, int STEPS, bool INTERLEAVED>
+template <typename T, int STEPS, bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(PA_BLOCK) void paged_append_kernel(AppendArgs a)
 {
     typedef typename Elem<T>::Raw Raw;
@@ -68,8 +68,8 @@ __global__ __launch_bounds__(PA_BLOCK) void paged_append_kernel(AppendArgs a)
             const T *src = r < a.HG ? (const T *)a.q + token * a.q_stride + (int64_t)r * HEAD_DIM
                          : r < a.HG + a.H ? (const T *)a.k + token * a.k_stride + (int64_t)(r - a.HG) * HEAD_DIM
                                           : (const T *)a.v + token * a.v_stride + (int64_t)(r - a.HG - a.H) * HEAD_DIM;
-            x0[i] = Elem<T>::load(src, c0);
-            x1[i] = Elem<T>::load(src, c1);
+            x0[i] = STREAM ? Elem<T>::load_stream(src, c0) : Elem<T>::load(src, c0);
+            x1[i] = STREAM ? Elem<T>::load_stream(src, c1) : Elem<T>::load(src, c1);
         }
     }
     const int64_t slot = (int64_t)min(max(a.past_lens[b], 0), cap) + t;
@@ -119,22 +119,33 @@ __global__ __launch_bounds__(PA_BLOCK) void paged_append_kernel(AppendArgs a)
             const int h = r < a.HG + a.H ? r - a.HG : r - a.HG - a.H;
             dst = (T *)(r < a.HG + a.H ? a.K : a.V) + ((((int64_t)page * a.H + h) << a.page_shift) + in_page) * HEAD_DIM;
         }
-        Elem<T>::store(dst, c0, x0[i]);
-        Elem<T>::store(dst, c1, x1[i]);
+        if (STREAM) {
+            Elem<T>::store_stream(dst, c0, x0[i]);
+            Elem<T>::store_stream(dst, c1, x1[i]);
+        } else {
+            Elem<T>::store(dst, c0, x0[i]);
+            Elem<T>::store(dst, c1, x1[i]);
+        }
     }
 }
 
 template <typename T>
 static kvm_status launch_t(AppendArgs &a, bool interleaved, hipStream_t st)
 {
-    constexpr int STEPS = 2;
     const int rows = a.HG + 2 * a.H;
-    a.groups = (rows + 8 * STEPS - 1) / (8 * STEPS);
-    a.token_blocks = (int)(((int64_t)a.B * a.T * a.groups + PA_WAVES - 1) / PA_WAVES);
-    const dim3 grid((unsigned)(a.token_blocks + (a.B + PA_BLOCK - 1) / PA_BLOCK));
     ProfScope prof("paged_append_kernel", st);
-    if (interleaved) hipLaunchKernelGGL((paged_append_kernel<T, STEPS, true>), grid, dim3(PA_BLOCK), 0, st, a);
-    else hipLaunchKernelGGL((paged_append_kernel<T, STEPS, false>), grid, dim3(PA_BLOCK), 0, st, a);
+    const auto run = [&](auto kernel, int steps) {
+        a.groups = (rows + 8 * steps - 1) / (8 * steps);
+        a.token_blocks = (int)(((int64_t)a.B * a.T * a.groups + PA_WAVES - 1) / PA_WAVES);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(a.token_blocks + (a.B + PA_BLOCK - 1) / PA_BLOCK)), dim3(PA_BLOCK), 0, st, a);
+    };
+    // Steps that the last-level cache cannot hold carry the non-temporal hint, and a wave has eight rows instead of sixteen.  us, plain with 16 rows /
+    // hint with 16 / hint with 8: 16384 tokens of 40 heads in fp16 (1.0 GB) 190 / 181 / 172, 8192 in fp32 194 / 202 / 179; smaller ones
+    // differ by less than their runs do.
+    if ((int64_t)a.B * a.T * rows * HEAD_DIM * (int)sizeof(T) * 2 >= LLC_BYTES)
+        interleaved ? run(paged_append_kernel<T, 1, true, true>, 1) : run(paged_append_kernel<T, 1, false, true>, 1);
+    else
+        interleaved ? run(paged_append_kernel<T, 2, true, false>, 2) : run(paged_append_kernel<T, 2, false, false>, 2);
     return check_launch("paged_append_kernel");
 }
 

@@ -112,6 +112,37 @@ def test_append_sizes(dtype, B, T, H, G, page, new, past, pos, fused):
     _append_case(dtype, B, T, H, G, page, 128, False, new, past, pos, 2, fused)
 
 
+@pytest.mark.parametrize("dtype,B,T", [("f16", 3, 7000), ("f32", 2, 5500)])
+def test_append_of_more_than_the_last_level_cache(dtype, B, T):
+    """Large steps take the streaming kernel: rows of both ends against the plain form, and every value row against its source."""
+    H, G, page, tdt = 16, 2, 64, gu.TORCH_DT[dtype]
+    n_pages = B * (T // page + 2)
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.randn((B, T, (G + 2) * H, 128), generator=gen, device="cuda").to(tdt)
+    assert 2 * x.nbytes >= 256 << 20
+    Kp, Vp = (torch.full((n_pages, H, page, 128), MARK, dtype=tdt, device="cuda") for _ in range(2))
+    table = torch.randperm(n_pages, device="cuda").to(torch.int32).view(B, -1)
+    new, past, pos = [T, T - 77, 5][:B], [3, 0, 60][:B], [1000, 0, 7][:B]
+    pages = kb.make_pages(Kp, Vp, table)
+    freq = (1.0 / 10000.0 ** (np.arange(0, 128, 2) / 128)).astype(np.float32)
+    q_out, kv = torch.full((B, T, G * H, 128), MARK, dtype=tdt, device="cuda"), _i32([0] * B)
+    HG = G * H
+    kb.kvm_paged_append(kb.make_token_shape(pages, T, G, _i32(new)), pages, kb.make_rotation(torch.from_numpy(freq).cuda(), True), x[:, :, :HG],
+                        x[:, :, HG:HG + H], x[:, :, HG + H:], _i32(past), _i32(pos), q_out, kv)
+    assert kv.tolist() == [p + n for p, n in zip(past, new)]
+    assert (q_out[1, new[1]:] == MARK).all()
+    for b in range(B):
+        slot = past[b] + torch.arange(new[b], device="cuda")
+        where = table[b].long()[slot // page]
+        assert torch.equal(Vp[where, :, slot % page], x[b, :new[b], HG + H:])
+        for t in {0, 1, new[b] // 2, new[b] - 1}:
+            turned = ar.rotate(gu.to_host_f64(x[b, t, :HG + H]), np.full(HG + H, pos[b] + past[b] + t), freq, True)
+            got = torch.cat([q_out[b, t], Kp[where[t], :, slot[t] % page]])
+            length = np.repeat(np.hypot(*(gu.to_host_f64(x[b, t, :HG + H])[:, i::2] for i in (0, 1))), 2, axis=1)
+            half = ar.EPS[dtype] / 2
+            _check(got, turned, 2.0 ** -20 * length * (1 + 2 * half) + half * np.abs(turned) + ar.TINY[dtype], f"row {b} token {t}")
+
+
 def test_append_without_queries_and_in_place():
     _append_case("bf16", 3, 5, 2, 3, 16, 64, True, [5, 2, 0], [1, 14, 3], [7, 8, 9], 3, queries=False)
     _append_case("f16", 3, 5, 2, 3, 16, 64, False, [5, 2, 0], [1, 14, 3], [7, 8, 9], 4, fused=False, in_place=True)
