@@ -270,6 +270,10 @@ template <typename T> struct WideLoad {
         if (n - j0 < 64) there &= (1ull << (n - j0)) - 1;
         const int64_t at_row = (((int64_t)page * a.H + h) << shift) + (j & ((1 << shift) - 1));
         const uint32_t lo = (uint32_t)at_row, hi = (uint32_t)(at_row >> 32);
+        if (shift >= 6 && there == ~0ull) {                   // one page has them all, one after the other
+            const uint64_t first = (((uint64_t)__builtin_amdgcn_readfirstlane(hi) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane(lo)) * KT::ROWB;
+            return prefix((const char *)a.Kt + first, (const char *)a.Vt + first, 0, 64, kt, vt);
+        }
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
