@@ -463,6 +463,8 @@ def _token_stride(name, t, want, dtype, current):
     if t.get_device() != current:
         raise ValueError(f"{name} is not on the current GPU")
     B, T, heads, d = want
+    if B * T == 0:
+        return heads * d
     row, token, head, elem = t.stride()
     if T == 1:
         token = row if B > 1 else heads * d

@@ -164,7 +164,7 @@ static kvm_status check_rows(const kvm_shape *sh, const char *fn, const char *na
     return KVM_OK;
 }
 
-static kvm_status check_pages(const kvm_pages *pg, const char *fn)
+static kvm_status check_pages(const kvm_shape *sh, const kvm_pages *pg, const char *fn)
 {
     if (pg->n_pages < 0 || pg->max_pages < 0 || pg->page_size < 1 || pg->page_size > 65536 || (pg->page_size & (pg->page_size - 1)) != 0) {
         set_error("%s: invalid pages (n_pages=%d, max_pages=%d, page_size=%d, a power of two up to 65536)", fn, pg->n_pages, pg->max_pages,
@@ -175,7 +175,7 @@ static kvm_status check_pages(const kvm_pages *pg, const char *fn)
         set_error("%s: a row of %d pages of %d tokens is too long", fn, pg->max_pages, pg->page_size);
         return KVM_ERR_UNSUPPORTED;
     }
-    if ((pg->n_pages > 0 && (!pg->K || !pg->V)) || (pg->max_pages > 0 && !pg->table) || !aligned16(pg->K) || !aligned16(pg->V)) {
+    if ((pg->n_pages > 0 && (!pg->K || !pg->V)) || (sh->B > 0 && pg->max_pages > 0 && !pg->table) || !aligned16(pg->K) || !aligned16(pg->V)) {
         set_error("%s: the pages' K, V and table must not be NULL, K and V multiples of 16 bytes", fn);
         return KVM_ERR_INVALID_ARG;
     }
@@ -470,7 +470,7 @@ kvm_status kvm_paged_append(const kvm_shape *shape, const kvm_pages *pages, cons
     kvm_status rc = check_shape(shape, fn);
     if (rc != KVM_OK) return rc;
     if (!pages || !rotation) { set_error("%s: pages and rotation must not be NULL", fn); return KVM_ERR_INVALID_ARG; }
-    rc = check_pages(pages, fn);
+    rc = check_pages(shape, pages, fn);
     if (rc == KVM_OK) rc = check_tokens(shape, fn);
     if (rc != KVM_OK) return rc;
     if (rotation->rot_dim < 0 || rotation->rot_dim > HEAD_DIM || rotation->rot_dim % 16 != 0) {
@@ -510,7 +510,7 @@ static kvm_status check_attn_sources(const kvm_shape *shape, const kvm_prefix *p
     if (!prefix && !pages) { set_error("%s: prefix and pages must not both be NULL", fn); return KVM_ERR_INVALID_ARG; }
     rc = check_tokens(shape, fn);
     if (rc == KVM_OK && prefix) rc = check_prefix(shape, prefix, fn);
-    if (rc == KVM_OK && pages) rc = check_pages(pages, fn);
+    if (rc == KVM_OK && pages) rc = check_pages(shape, pages, fn);
     return rc;
 }
 
@@ -537,6 +537,7 @@ kvm_status kvm_prefix_attn(const kvm_shape *shape, const kvm_prefix *prefix, con
         set_error("%s: workspace of %zu bytes needed, %zu given", fn, need, ws ? ws_bytes : (size_t)0);
         return KVM_ERR_WORKSPACE;
     }
+    if (!aligned16(ws)) { set_error("%s: the workspace must be 256-byte aligned", fn); return KVM_ERR_INVALID_ARG; }
     return launch_prefix_attn(*shape, prefix, pages, Q, q_stride, kv_lens, out, lse_opt, ws, (hipStream_t)stream);
 }
 

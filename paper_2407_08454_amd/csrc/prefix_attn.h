@@ -341,47 +341,72 @@ template <typename T> struct Queries {
     }
 };
 
-// One token at a time, for the tiles that values() may not touch (see has_nonfinite): the same state, every lane its own query and half
-// of the dimensions; a query that does not see the token leaves it out altogether.  A call of its own, on a copy of the accumulators in
-// memory: as part of the kernels it took the registers of their loops (8 x 2048 new tokens 2.46 -> 2.97 ms).
+// One key at a time, where infinities or NaN among the values must not meet a weight of zero (what a query does not see) or the rest of a
+// rounded weight: every lane its own query and half of the dimensions; a query that does not see the key leaves it out altogether.  Rare, and a
+// call of its own on a copy of the accumulators: inlined it took the registers of the tile loops (8 x 2048 new tokens 2.46 -> 2.97 ms).
 struct LaneState { float o[4][16], m, l; };
-struct TokenSource { const void *K, *V; const int32_t *table; int n_pages, page_shift, H, h; float c; };
+struct KeySource { const void *K, *V; const int32_t *table; int n_pages, page_shift, H, h; float c; };   // table NULL: K and V are a list of rows
 template <typename T>
-static __device__ __attribute__((noinline)) void one_by_one(LaneState *st, TokenSource src, const T *q, int sees, int first, int last)
+static __device__ __attribute__((noinline)) void one_by_one(LaneState *st, KeySource src, const T *q, int sees, int first, int last)
 {
     const int hf = (threadIdx.x >> 5) & 1;
+    float o[4][16], m = st->m, l = st->l;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = st->o[d][i];
     for (int j = first; j < last; ++j) {
-        const int page = src.table[j >> src.page_shift];
-        if (page < 0 || page >= src.n_pages) continue;
-        const size_t at = ((((size_t)page * src.H + src.h) << src.page_shift) + (j & ((1 << src.page_shift) - 1))) * HEAD_DIM;
-        const T *kr = (const T *)src.K + at + 64 * hf, *vr = (const T *)src.V + at;
+        size_t at = j;
+        if (src.table) {
+            const int page = src.table[j >> src.page_shift];
+            if (page < 0 || page >= src.n_pages) continue;
+            at = (((size_t)page * src.H + src.h) << src.page_shift) + (j & ((1 << src.page_shift) - 1));
+        }
+        const T *kr = (const T *)src.K + at * HEAD_DIM + 64 * hf, *vr = (const T *)src.V + at * HEAD_DIM + 4 * hf;
         float s = 0.f;
-#pragma unroll 1
+#pragma unroll
         for (int f = 0; f < 8; ++f) s += RowDot<T>::dot(Elem<T>::load(kr, f), Elem<T>::load(q + 64 * hf, f));
         s = (s + other_half(s)) * src.c;
         if (j >= sees) continue;
-        const float next = fmaxf(st->m, s), scale = __builtin_amdgcn_exp2f(st->m - next), w = __builtin_amdgcn_exp2f(s - next);
-        st->l = st->l * scale + (hf ? 0.f : w);               // (the halves' sums are added in the end)
-        st->m = next;
-#pragma unroll 1
+        const float next = fmaxf(m, s), scale = __builtin_amdgcn_exp2f(m - next), w = __builtin_amdgcn_exp2f(s - next);
+        l = l * scale + (hf ? 0.f : w);                       // (the halves' sums are added in the end)
+        m = next;
+#pragma unroll
         for (int d = 0; d < 4; ++d)
-#pragma unroll 1
-            for (int i = 0; i < 16; ++i) st->o[d][i] = st->o[d][i] * scale + w * (float)vr[32 * d + 8 * (i >> 2) + 4 * hf + (i & 3)];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                T v[4];
+                __builtin_memcpy(v, vr + 32 * d + 8 * i, sizeof(v));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[d][4 * i + e] = o[d][4 * i + e] * scale + w * (float)v[e];
+            }
     }
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st->o[d][i] = o[d][i];
+    st->m = m;
+    st->l = l;
 }
-// tokens [first, last) of row b for a wave's queries
+// keys [first, last) of prefix (p, h), or, p < 0, tokens of row b, for a wave's queries; afresh: instead of what they have
 template <typename T>
-__device__ __forceinline__ void one_by_one(const PrefixAttnArgs &a, Queries<T> &qs, int b, int h, int first, int last) {
+__device__ __forceinline__ void one_by_one(const PrefixAttnArgs &a, Queries<T> &qs, int p, int b, int h, int first, int last, bool afresh) {
     LaneState st;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) st.o[d][i] = qs.o[d][i];
-    st.m = qs.m;
-    st.l = qs.l;
-    const int64_t HG = a.H * a.G, token = qs.valid ? qs.row / HG : (int64_t)b * a.T, head = qs.valid ? qs.row - token * HG : h * a.G;
-    const TokenSource src = {a.Kt, a.Vt, a.table + (size_t)b * a.max_pages, a.n_pages, a.page_shift, a.H, h, a.c};
-    one_by_one<T>(&st, src, (const T *)a.q + token * a.q_stride + head * HEAD_DIM, qs.valid ? qs.sees : 0, first, last);
+        for (int i = 0; i < 16; ++i) st.o[d][i] = afresh ? 0.f : qs.o[d][i];
+    st.m = afresh ? PX_NONE : qs.m;
+    st.l = afresh ? 0.f : qs.l;
+    const int64_t HG = a.H * a.G, token = qs.valid ? qs.row / HG : 0, head = qs.valid ? qs.row - token * HG : 0;
+    KeySource src = {a.Kt, a.Vt, a.table + (size_t)b * a.max_pages, a.n_pages, a.page_shift, a.H, h, a.c};
+    if (p >= 0) {
+        const size_t at = ((size_t)p * a.H + h) * a.cap * HEAD_DIM;
+        src.K = (const T *)a.Kp + at;
+        src.V = (const T *)a.Vp + at;
+        src.table = nullptr;
+    }
+    one_by_one<T>(&st, src, (const T *)a.q + token * a.q_stride + head * HEAD_DIM, !qs.valid ? 0 : p >= 0 ? last : qs.sees, first, last);
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll

@@ -174,7 +174,6 @@ __device__ __forceinline__ void split_unit(const PrefixAttnArgs &a, int u, u32x4
     load(K, kt);
     load(V, vt);
     qs.init(a, lin + (lane & 31), lin_end, h);
-    int stop = end;                                          // tokens from here on one at a time
     for (int j = j0; j < end; j += 32) {
         const uint32_t there = next;
         wait_vmcnt<KT::LOADS>();
@@ -190,7 +189,6 @@ __device__ __forceinline__ void split_unit(const PrefixAttnArgs &a, int u, u32x4
         const bool mixed = tail && j + 32 > least;
         if (mixed || there != 0xFFFFFFFFu) {
             qs.mask(x, there, tail ? qs.sees - j : 32);
-            if (mixed && a.T > 1 && has_nonfinite<T>(vt)) { stop = j; break; }
         }
         qs.weights(x, a.c);
         qs.template values<true>(tl, x, vt);
@@ -198,7 +196,14 @@ __device__ __forceinline__ void split_unit(const PrefixAttnArgs &a, int u, u32x4
         if (j + 32 < end) load(V, vt);
     }
     wait_vmcnt<0>();
-    if (stop < end) one_by_one<T>(a, qs, b, h, stop, end);   // (tails only)
+    // Infinities or NaN among the values: the part once more, key by key.  They may be behind a mask, or make a NaN of an infinity with the rest
+    // of its weight.
+    float finite = 0.f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) finite = fmaf(qs.o[d][i], 0.f, finite);
+    if (__ballot(qs.valid && finite != 0.f)) one_by_one<T>(a, qs, tail ? -1 : p, b, h, j0, end, true);
 
     const float l = qs.l + other_half(qs.l);
     if (!qs.valid) return;
@@ -389,7 +394,7 @@ __global__ __launch_bounds__(4 * WAVE, 2) void prefix_attn_wide_kernel(PrefixAtt
             if (++v >= v_end) break;
         }
     }
-    if (ROWS && !idle && stop < tail_end) one_by_one<T>(a, qs, b, h, stop, tail_end);
+    if (ROWS && !idle && stop < tail_end) one_by_one<T>(a, qs, -1, b, h, stop, tail_end, false);
     const float l = qs.l + other_half(qs.l);
     if (!qs.valid) return;
     if (ROWS && splits == 1) {

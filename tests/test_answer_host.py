@@ -101,6 +101,7 @@ def test_append_refuses(kw, code, word):
     (dict(kv=None), kb.KVM_ERR_INVALID_ARG, "kv_lens"),
     (dict(ws=None), kb.KVM_ERR_WORKSPACE, "workspace"),
     (dict(nbytes=16), kb.KVM_ERR_WORKSPACE, "workspace"),
+    (dict(ws=ctypes.c_void_p(4100)), kb.KVM_ERR_INVALID_ARG, "aligned"),
 ])
 def test_attention_refuses(kw, code, word):
     assert _attn(**kw) == code and word in _message()
@@ -115,7 +116,9 @@ def test_null_descriptors_and_nothing_to_do():
     assert lib.kvm_paged_append(ctypes.byref(sh), None, ctypes.byref(rot), *args) == kb.KVM_ERR_INVALID_ARG
     assert lib.kvm_paged_append(ctypes.byref(sh), ctypes.byref(pg), None, *args) == kb.KVM_ERR_INVALID_ARG
     assert _append(shape=_shape(B=0), q=None, k=None, v=None, past=None, kv=None, q_out=None) == kb.KVM_OK
+    assert _append(shape=_shape(B=0), pages=_pages(table=None), q=None, k=None, v=None, past=None, kv=None, q_out=None) == kb.KVM_OK
     assert _attn(shape=_shape(B=0), q=None, out=None, ws=None) == kb.KVM_OK
+    assert _attn(shape=_shape(B=0), pages=_pages(table=None), q=None, out=None, ws=None) == kb.KVM_OK
     assert _attn(shape=_shape(N=0), q=None, out=None, ws=None) == kb.KVM_OK
     assert lib.kvm_prefix_attn(None, None, ctypes.byref(pg), ONE, 1024, ONE, ONE, None, ONE, 1 << 30, None) == kb.KVM_ERR_INVALID_ARG
     assert lib.kvm_prefix_attn_workspace_bytes(None, None, ctypes.byref(pg)) == 0

@@ -364,6 +364,52 @@ def test_a_later_token_has_no_influence(dtype, T, G, value):
     _check(a.lse[:, :last], lse, l_tol, "lse")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,rows", [(1, 3), (1, 200), (5, 3), (150, 2)])
+def test_an_infinite_value_that_is_seen_stays_infinite(dtype, T, rows):
+    """One infinity among a prefix's values and one among a tail's: in their dimensions of the queries that see them, nowhere else."""
+    _say(f"infinite value {dtype} T={T} rows={rows}")
+
+    def spoil(table, n_pages, K, V):
+        V[table[1, 0], 1, 2, 5] = -np.inf                      # token 2 of row 1, KV head 1
+
+    a = Attn(dtype, rows, T, 2, 2, 15, P=1, cap=90, lens=[[90, 70]], kv=[T + 40] * rows, spoil=spoil)
+    a.prefix64["V"][0, 0, 33, 7] = np.inf
+    a.prefix._refs[1][0, 0, 33, 7] = float("inf")
+    a.run()
+    few = min(rows, 3)
+    out, lse, bounds = ar.attention(a.q64[:few], 2, None, a.prefix64, dict(a.pages64, table=a.pages64["table"][:few], kv_lens=a.pages64["kv_lens"][:few]))
+    o_tol, l_tol = ar.tolerance(dtype, out, lse, tuple(np.nan_to_num(x, posinf=0.0) for x in bounds))
+    assert np.isposinf(out[:, :, :2, 7]).all() and np.isneginf(out[1, :, 2:, 5]).all() and np.isinf(out).sum() == few * T * 2 + T * 2
+    _check(a.out[:few], out, o_tol, "out")
+    _check(a.lse[:few], lse, l_tol, "lse")
+
+
+def test_steps_without_tokens_and_batches_without_rows():
+    tdt = torch.float16
+    pool = [torch.full((3, 2, 4, 128), MARK, dtype=tdt, device="cuda") for _ in range(2)]
+    empty = lambda *s: torch.empty(s, dtype=tdt, device="cuda")
+    pages = kb.make_pages(*pool, _i32([[0, 1], [2, -1]]))
+    shape, kv = kb.make_token_shape(pages, 0, 2), _i32([-1, -1])
+    kb.kvm_paged_append(shape, pages, kb.make_rotation(), empty(2, 0, 4, 128), empty(2, 0, 2, 128), empty(2, 0, 2, 128), _i32([5, 3]), None,
+                        empty(2, 0, 4, 128), kv)
+    assert kv.tolist() == [5, 3] and all((t == MARK).all() for t in pool)
+    ws = torch.empty(kb.kvm_prefix_attn_workspace_bytes(shape, None, pages), dtype=torch.uint8, device="cuda")
+    kb.kvm_prefix_attn(shape, None, pages, empty(2, 0, 4, 128), kv, empty(2, 0, 4, 128), None, ws)
+    none = kb.make_pages(*pool, torch.empty((0, 2), dtype=torch.int32, device="cuda"))
+    shape, kv = kb.make_token_shape(none, 3, 2), torch.empty(0, dtype=torch.int32, device="cuda")
+    kb.kvm_paged_append(shape, none, kb.make_rotation(), empty(0, 3, 4, 128), empty(0, 3, 2, 128), empty(0, 3, 2, 128), kv, None,
+                        empty(0, 3, 4, 128), torch.empty(0, dtype=torch.int32, device="cuda"))
+    kb.kvm_prefix_attn(shape, None, none, empty(0, 3, 4, 128), kv, empty(0, 3, 4, 128), None, ws)
+    torch.cuda.synchronize()
+    # pools and tables without pages: nothing to see
+    bare = kb.make_pages(empty(0, 2, 4, 128), empty(0, 2, 4, 128), torch.empty((2, 0), dtype=torch.int32, device="cuda"))
+    shape, out = kb.make_token_shape(bare, 1, 2), torch.full((2, 1, 4, 128), MARK, dtype=tdt, device="cuda")
+    ws = torch.empty(kb.kvm_prefix_attn_workspace_bytes(shape, None, bare), dtype=torch.uint8, device="cuda")
+    kb.kvm_prefix_attn(shape, None, bare, torch.ones_like(out), _i32([9, 9]), out, None, ws)
+    assert (out == 0).all()
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_attention_with_equal_scores_is_the_mean(dtype):
     """Queries of zero: the plain mean of the values, whatever the number of keys; the log-sum-exp counts them."""
