@@ -628,7 +628,8 @@ static kvm_status launch_t(const PrefixAttnArgs &a, hipStream_t st)
     const int parts = a.splits_p + a.splits_t;
     if (parts <= JOIN_AHEAD) join(prefix_attn_join_kernel<T, 1>, 1);
     else if (parts <= 2 * JOIN_AHEAD) join(prefix_attn_join_kernel<T, 2>, 2);
-    else if (parts <= 4 * JOIN_AHEAD) join(prefix_attn_join_kernel<T, 4>, 4);
+    // (eight groups where rows are few; 2048 rows of 20 parts, us, by eight / four / two groups 9.0 / 7.9 / 8.7, 32 of 34 5.5 / 7.2 / 10.1)
+    else if (parts <= 4 * JOIN_AHEAD || query_rows(a) > 1024) join(prefix_attn_join_kernel<T, 4>, 4);
     else join(prefix_attn_join_kernel<T, 8>, 8);
     return check_launch("prefix_attn_join_kernel");
 }
