@@ -286,6 +286,12 @@ CASES = {
     "long_prefix": dict(B=2, T=1, H=1, G=1, P=1, cap=20011, kv=[1, 40]),
     "long_tail": dict(B=2, T=1, H=1, G=2, P=1, cap=10, kv=[9001, 317], page=128),
     "long_both_t2": dict(B=2, T=2, H=1, G=1, P=2, cap=5000, lens=[[5000], [4097]], kv=[6000, 2], page=64),
+    # pages of one token (a tile takes as many entries of the table as are held at once), pages longer than most rows
+    "pages_of_one": dict(B=3, T=1, H=2, G=1, P=1, cap=10, kv=[500, 64, 65], page=1),
+    "pages_of_one_chunk": dict(B=2, T=140, H=1, G=1, P=1, cap=70, kv=[300, 141], page=1),
+    "pages_of_two_chunk": dict(B=1, T=70, H=1, G=2, kv=[401], page=2),
+    "long_pages": dict(B=2, T=1, H=1, G=2, kv=[1500, 3], page=1024),
+    "long_pages_chunk": dict(B=2, T=150, H=1, G=1, P=1, cap=64, kv=[1100, 150], page=1024),
     # a prefix alone (another length than the queries'), pages alone
     "prefix_alone": dict(B=3, T=50, H=2, G=2, P=3, cap=333, lens=[[333, 100], [1, 0], [32, 33]], new=[50, 20, 3]),
     "pages_alone": dict(B=5, T=1, H=3, G=2, kv=[1, 16, 17, 0, 500]),
