@@ -14,7 +14,12 @@
 namespace kvm {
 
 constexpr float PX_NONE = -3.0e38f;      // maximum of no score: finite, so that no inf - inf arises
-constexpr float PX_SLACK = 8.f;          // weights may reach 2^8 before a query's accumulators are put on a new maximum
+
+// Weights are exp2(score - reference).  The reference is put PX_LIFT below the maximum, and again when a score lies more than PX_SLACK above that,
+// so that the accumulators are rarely scaled.  fp16: weights below 2^-25 are lost, and beside a first state that takes nearly all of the weight
+// thousands of them are the output: with weights of up to 2^15 only what is below 2^-35 of the greatest is.
+template <typename T> constexpr float PX_LIFT = Elem<T>::kDtype == KVM_F16 ? 10.f : 0.f;
+template <typename T> constexpr float PX_SLACK = Elem<T>::kDtype == KVM_F16 ? 5.f : 8.f;
 
 enum { PX_WIDE_NONE = 0, PX_WIDE_ROWS = 1, PX_WIDE_PREFIX = 2 };
 
@@ -252,12 +257,12 @@ template <typename T> struct Queries {
         }
     }
 
-    // the tile's weights, taken against a reference that may lag behind the maximum by PX_SLACK
+    // the tile's weights, taken against a reference that lags behind the maximum
     __device__ __forceinline__ void weights(f32x16 &s, float c) {
         float top = max16(s);
         top = fmaxf(top, other_half(top)) * c;
-        if (__ballot(top > m + PX_SLACK)) {
-            const float next = fmaxf(m, top), scale = __builtin_amdgcn_exp2f(m - next);
+        if (__ballot(top > m + (PX_LIFT<T> + PX_SLACK<T>))) {
+            const float next = fmaxf(m, top - PX_LIFT<T>), scale = __builtin_amdgcn_exp2f(m - next);
             l *= scale;
 #pragma unroll
             for (int d = 0; d < 4; ++d)
@@ -277,8 +282,8 @@ template <typename T> struct Queries {
     __device__ __forceinline__ void weights(f32x16 &s0, f32x16 &s1, float c) {
         float top = fmaxf(max16(s0), max16(s1));
         top = fmaxf(top, other_half(top)) * c;
-        if (__ballot(top > m + PX_SLACK)) {
-            const float next = fmaxf(m, top), scale = __builtin_amdgcn_exp2f(m - next);
+        if (__ballot(top > m + (PX_LIFT<T> + PX_SLACK<T>))) {
+            const float next = fmaxf(m, top - PX_LIFT<T>), scale = __builtin_amdgcn_exp2f(m - next);
             l *= scale;
 #pragma unroll
             for (int d = 0; d < 4; ++d)

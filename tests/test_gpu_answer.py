@@ -391,6 +391,30 @@ def test_an_infinite_value_that_is_seen_stays_infinite(dtype, T, rows):
     _check(a.lse[:few], lse, l_tol, "lse")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,rows", [(1, 2), (1, 200), (150, 2)])
+def test_many_small_weights_beside_a_great_one(dtype, T, rows):
+    """A first state with nearly all of the weight and a value of zero, as models have them: the output is what thousands of weights of
+    e^-18 leave.  In fp16 a weight is off by 2^-25 at most where the greatest is 2^10 or more, so by 2^-35 of the greatest."""
+    _say(f"small weights {dtype} T={T} rows={rows}")
+    n = 4000
+    a = Attn(dtype, rows, T, 1, 1, 16, P=1, cap=n)
+    a.prefix64["K"][...] = 0.0
+    a.prefix64["K"][0, 0, 0, 0] = 14.25                       # 14.25^2 / sqrt(128) = 17.95
+    a.prefix64["V"][...] = 64.0 + np.arange(128) / 2
+    a.prefix64["V"][0, 0, 0] = 0.0
+    a.q64[...] = 0.0
+    a.q64[..., 0] = 14.25
+    for x64, x in ((a.prefix64["K"], a.prefix._refs[0]), (a.prefix64["V"], a.prefix._refs[1]), (a.q64, a.q)):
+        x.copy_(torch.from_numpy(x64))                        # (exact in every type)
+    a.run()
+    few = min(rows, 2)
+    out, lse, (spread, worst, small) = ar.attention(a.q64[:few], 1, None, a.prefix64, None)
+    o_tol, l_tol = ar.tolerance(dtype, out, lse, (spread, worst, small * 2.0 ** -10))
+    _check(a.out[:few], out, o_tol, "out")
+    _check(a.lse[:few], lse, l_tol, "lse")
+
+
 def test_steps_without_tokens_and_batches_without_rows():
     tdt = torch.float16
     pool = [torch.full((3, 2, 4, 128), MARK, dtype=tdt, device="cuda") for _ in range(2)]
