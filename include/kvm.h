@@ -438,6 +438,8 @@ typedef struct {
  *   kv_lens   out  [B] past + new, not beyond max_pages*page_size: what kvm_prefix_attn reads, and past_lens of
  *                  the next call.  A buffer of its own, not past_lens.
  * A token whose page the row does not have (see kvm_pages) or whose slot lies behind the table is not stored.
+ * (A row that outgrows its table has to end: kv_lens stops at the table's end, and kvm_prefix_attn counts the step's tokens back
+ * from there.)
  * Slots that are written in one call have to be different memory: two rows of a batch may share pages that
  * they only read.  The call needs no workspace.
  */

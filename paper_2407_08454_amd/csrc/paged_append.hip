@@ -77,6 +77,7 @@ __global__ __launch_bounds__(PA_BLOCK) void paged_append_kernel(AppendArgs a)
     if (slot < cap) page = a.table[(int64_t)b * a.max_pages + (slot >> a.page_shift)];
     const int64_t x = slot + (a.pos_base ? a.pos_base[b] : 0);
     if (lane < a.rot / 2) units[wave][lane] = unit_at(x, a.inv_freq[lane]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");    // (a wave's LDS operations stay in order: it holds the compiler)
     __builtin_amdgcn_wave_barrier();
     float2 w[8];
     if (turns) {
