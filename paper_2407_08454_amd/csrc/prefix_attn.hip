@@ -544,6 +544,7 @@ static void plan(const kvm_shape &sh, const kvm_prefix *prefix, const kvm_pages 
 {
     a.B = sh.B; a.T = sh.N; a.H = sh.H_kv; a.G = sh.G; a.new_lens = sh.seq_lens;
     const int64_t per_row = (int64_t)a.T * a.G;
+    if (a.B * per_row == 0) return;                          // no query: nothing is launched, and below units are divided by
     if (prefix && prefix->P > 0 && prefix->capacity > 0) {
         a.Kp = prefix->K; a.Vp = prefix->V; a.lens = prefix->lens; a.row_start = prefix->row_start; a.P = prefix->P; a.cap = prefix->capacity;
     }

@@ -128,6 +128,20 @@ def test_null_descriptors_and_nothing_to_do():
         kb.kvm_prefix_attn_workspace_bytes(sh, None, None)
 
 
+@pytest.mark.parametrize("dtype", [kb.KVM_F32, kb.KVM_F16, kb.KVM_BF16])
+@pytest.mark.parametrize("B,N", [(0, 1), (0, 3), (0, 32), (0, 200), (0, 0), (4, 0)])
+@pytest.mark.parametrize("G", [1, 4])
+@pytest.mark.parametrize("sources", ["both", "prefix", "pages", "no table", "row_start"])
+def test_workspace_of_batches_without_rows_and_steps_without_tokens(dtype, B, N, G, sources):
+    """Such a call has nothing to keep: the least size, whichever kernels a row or a token more would take."""
+    prefix = None if sources in ("pages", "no table") else _prefix(row_start=4096 if sources == "row_start" else None)
+    pages = None if sources == "prefix" else _pages(table=4096 if B or sources != "no table" else None)
+    sizes = dict(dtype=dtype, G=G)
+    assert kb.kvm_prefix_attn_workspace_bytes(_shape(B=B, N=N, **sizes), prefix, pages) == 256
+    assert kb.kvm_prefix_attn_workspace_bytes(_shape(B=4, N=max(N, 1), **sizes), prefix, _pages()) >= 256
+    assert _attn(shape=_shape(B=B, N=N, **sizes), prefix=prefix, pages=pages, q=None, out=None, kv=None, ws=None, nbytes=0) == kb.KVM_OK
+
+
 def test_descriptors_have_the_layout_of_the_header(tmp_path):
     structs = {"kvm_pages": kb.KvmPages, "kvm_rotation": kb.KvmRotation, "kvm_prefix": kb.KvmPrefix}
     lines = ['#include <stddef.h>', '#include <stdio.h>', '#include "kvm.h"', 'int main(void) {']

@@ -440,6 +440,16 @@ def test_steps_without_tokens_and_batches_without_rows():
     assert (out == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,G", [(1, 1), (3, 2), (200, 1)])
+def test_a_batch_without_rows_with_the_workspace_of_its_own_size(dtype, T, G):
+    """A running batch whose last row has ended: sized, and called, as any other."""
+    _say(f"no rows {dtype} T={T} G={G}")
+    a = Attn(dtype, 0, T, 2, G, 17, P=1, cap=50, lens=[[50, 7]], row_start=[0, 0], kv=[])
+    assert a.ws.numel() == 256
+    a.run()
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_attention_with_equal_scores_is_the_mean(dtype):
     """Queries of zero: the plain mean of the values, whatever the number of keys; the log-sum-exp counts them."""
