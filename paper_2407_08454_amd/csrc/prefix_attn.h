@@ -393,9 +393,10 @@ static __device__ __attribute__((noinline)) void one_by_one(LaneState *st, KeySo
     st->m = m;
     st->l = l;
 }
-// keys [first, last) of prefix (p, h), or, p < 0, tokens of row b, for a wave's queries; afresh: instead of what they have
+// states [first_p, last_p) of prefix (p, h) and tokens [first_t, last_t) of row b for a wave's queries; afresh: instead of what they have
 template <typename T>
-__device__ __forceinline__ void one_by_one(const PrefixAttnArgs &a, Queries<T> &qs, int p, int b, int h, int first, int last, bool afresh) {
+__device__ __forceinline__ void one_by_one(const PrefixAttnArgs &a, Queries<T> &qs, int p, int b, int h, int first_p, int last_p, int first_t, int last_t,
+                                           bool afresh) {
     LaneState st;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -404,20 +405,36 @@ __device__ __forceinline__ void one_by_one(const PrefixAttnArgs &a, Queries<T> &
     st.m = afresh ? PX_NONE : qs.m;
     st.l = afresh ? 0.f : qs.l;
     const int64_t HG = a.H * a.G, token = qs.valid ? qs.row / HG : 0, head = qs.valid ? qs.row - token * HG : 0;
-    KeySource src = {a.Kt, a.Vt, a.table + (size_t)b * a.max_pages, a.n_pages, a.page_shift, a.H, h, a.c};
-    if (p >= 0) {
-        const size_t at = ((size_t)p * a.H + h) * a.cap * HEAD_DIM;
-        src.K = (const T *)a.Kp + at;
-        src.V = (const T *)a.Vp + at;
-        src.table = nullptr;
+    const T *q = (const T *)a.q + token * a.q_stride + head * HEAD_DIM;
+    const size_t at = ((size_t)max(p, 0) * a.H + h) * a.cap * HEAD_DIM;
+#pragma unroll 1
+    for (int tail = 0; tail < 2; ++tail) {                    // (a loop, so that the call stands here once)
+        const int first = tail ? first_t : first_p, last = tail ? last_t : last_p;
+        if (first >= last) continue;
+        const KeySource src = {tail ? a.Kt : (const T *)a.Kp + at, tail ? a.Vt : (const T *)a.Vp + at,
+                               tail ? a.table + (size_t)b * a.max_pages : nullptr, a.n_pages, a.page_shift, a.H, h, a.c};
+        one_by_one<T>(&st, src, q, !qs.valid ? 0 : tail ? qs.sees : last, first, last);
     }
-    one_by_one<T>(&st, src, (const T *)a.q + token * a.q_stride + head * HEAD_DIM, !qs.valid ? 0 : p >= 0 ? last : qs.sees, first, last);
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) qs.o[d][i] = st.o[d][i];
     qs.m = st.m;
     qs.l = st.l;
+}
+
+// Infinities or NaN among the sums of weighted values of a wave's queries, whose weights themselves add up to a number: a value is infinite or NaN.  It
+// may be behind a mask, or its weight may have been rounded, to zero or with a rest of the other sign, and have made a NaN of an
+// infinity: the keys have to be taken one by one.
+template <typename T>
+__device__ __forceinline__ bool sums_broken(const Queries<T> &qs) {
+    float finite = 0.f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) finite = fmaf(qs.o[d][i], 0.f, finite);
+    const float l = qs.l + other_half(qs.l);
+    return __ballot(qs.valid && finite != 0.f && l - l == 0.f) != 0;
 }
 
 // Does the value tile hold an infinity or a NaN?  Where some queries of a tile see a key that others do not (later tokens of the same

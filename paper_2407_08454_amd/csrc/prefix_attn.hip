@@ -196,14 +196,7 @@ __device__ __forceinline__ void split_unit(const PrefixAttnArgs &a, int u, u32x4
         if (j + 32 < end) load(V, vt);
     }
     wait_vmcnt<0>();
-    // Infinities or NaN among the values: the part once more, key by key.  They may be behind a mask, or make a NaN of an infinity with the rest
-    // of its weight.
-    float finite = 0.f;
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) finite = fmaf(qs.o[d][i], 0.f, finite);
-    if (__ballot(qs.valid && finite != 0.f)) one_by_one<T>(a, qs, tail ? -1 : p, b, h, j0, end, true);
+    if (sums_broken(qs)) one_by_one<T>(a, qs, p, b, h, tail ? 0 : j0, tail ? 0 : end, tail ? j0 : 0, tail ? end : 0, true);
 
     const float l = qs.l + other_half(qs.l);
     if (!qs.valid) return;
@@ -394,7 +387,11 @@ __global__ __launch_bounds__(4 * WAVE, 2) void prefix_attn_wide_kernel(PrefixAtt
             if (++v >= v_end) break;
         }
     }
-    if (ROWS && !idle && stop < tail_end) one_by_one<T>(a, qs, -1, b, h, stop, tail_end, false);
+    const bool again = sums_broken(qs);                      // all of the part once more
+    if (again || (ROWS && !idle && stop < tail_end)) {
+        const int v_first = part * per_part, first_t = again ? 64 * max(v_first - tiles_n, 0) : stop;
+        one_by_one<T>(a, qs, p, b, h, 64 * v_first, again ? min(n, 64 * v_end) : 0, first_t, ROWS ? tail_end : 0, again);
+    }
     const float l = qs.l + other_half(qs.l);
     if (!qs.valid) return;
     if (ROWS && splits == 1) {

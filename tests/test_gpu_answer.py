@@ -392,6 +392,34 @@ def test_an_infinite_value_that_is_seen_stays_infinite(dtype, T, rows):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,rows,H", [(1, 3, 2), (1, 200, 2), (150, 2, 2), (130, 65, 4)])
+def test_an_infinite_value_under_a_small_weight_stays_infinite(dtype, T, rows, H):
+    """The same where the weight is e^-30 of the greatest, which 16 bits do not hold: one among a prefix's values, one in the tail of a row,
+    long before its new tokens.  The last shape goes straight to the output."""
+    _say(f"infinite value, small weight {dtype} T={T} rows={rows}")
+    a = Attn(dtype, rows, T, H, 1, 18, P=1, cap=150, kv=[T + 190] * rows)
+    put = lambda x64, x, at, value: (x64.__setitem__(at, value), x.__setitem__(at, value))
+    every = np.s_[:]
+    put(a.q64, a.q, every, 0.0)
+    put(a.q64, a.q, np.s_[..., 0], 14.25)
+    (pre_k, pre_v, _, _), (own_k, own_v, _) = a.prefix._refs, a.pages._refs
+    put(a.prefix64["K"], pre_k, every, 0.0)
+    put(a.pages64["K"], own_k, every, 0.0)
+    put(a.prefix64["K"], pre_k, np.s_[:, :, 0, 0], 24.0)       # 14.25 * 24 / sqrt(128) = 30.2
+    put(a.prefix64["V"], pre_v, np.s_[0, 0, 133, 7], np.inf)
+    put(a.pages64["V"], own_v, np.s_[a.pages64["table"][1, 4], 1, 2, 5], -np.inf)      # token 66 of row 1, KV head 1
+    a.run()
+    assert (a.out == MARK).sum() == 0
+    few = 2 if T > 1 else 3
+    out, lse, bounds = ar.attention(a.q64[:few], 1, None, a.prefix64, dict(a.pages64, table=a.pages64["table"][:few], kv_lens=a.pages64["kv_lens"][:few]))
+    o_tol, l_tol = ar.tolerance(dtype, out, lse, tuple(np.nan_to_num(x, posinf=0.0) for x in bounds))
+    assert np.isposinf(out[:, :, 0, 7]).all() and np.isneginf(out[1, :, 1, 5]).all() and np.isinf(out).sum() == few * T + T
+    _check(a.out[:few], out, o_tol, "out")
+    _check(a.lse[:few], lse, l_tol, "lse")
+    assert torch.isinf(a.out).sum().item() == rows * T + T and not torch.isnan(a.out).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("T,rows", [(1, 2), (1, 200), (150, 2)])
 def test_many_small_weights_beside_a_great_one(dtype, T, rows):
     """A first state with nearly all of the weight and a value of zero, as models have them: the output is what thousands of weights of
