@@ -465,8 +465,7 @@ kvm_status kvm_paged_append(const kvm_shape *shape, const kvm_pages *pages, cons
  *   lse_opt   out  (B, T, H_kv*G) float32 or NULL
  *   ws        kvm_prefix_attn_workspace_bytes(), 256-byte aligned; one call at a time
  * Scores, sums and outputs are accumulated in fp32.  16-bit types: the weights exp(score - reference) meet the values as
- * two numbers of dtype, the rounded weight and what the rounding left; where 128 queries are worked on at a time (128 of a row's,
- * T * G, or on average of a prompt's) as the rounded one alone, half a step of a weight; fp16 weights are off by up to 2^-35 of the
+ * two numbers of dtype, the rounded weight and what the rounding left; fp16 weights are off by up to 2^-35 of the
  * greatest one besides, the end of that type's range.  Deterministic: no atomics, and a call on the same shape repeats its
  * bits.  The order of the sums follows from the sizes in shape, prefix and pages and from the lengths, so a row in another batch
  * can differ in its last bits.

@@ -299,10 +299,12 @@ template <typename T> struct Queries {
         l += p0 + p1;
     }
 
-    // O^T += V^T P^T.  With REST the weights go in as two numbers of the cache type, rounded and what the rounding left, so that all of the
-    // output's error is its own rounding; without, half a step of every weight is added to it (bf16, N(0, 1): 2.3e-3 of the output
-    // instead of 1.7e-3).  Where keys and values are waited for the second product costs nothing.
-    template <bool REST> __device__ __forceinline__ void values(const TileLane<T> &tl, const f32x16 &w, const u32x4 *vt) {
+    // O^T += V^T P^T.  The weights go in as two numbers of the cache type, rounded and what the rounding left, so that all of the output's
+    // error is its own rounding.  The rounded weight alone would add half a step of every weight: bf16, N(0, 1), 2.3e-3 of the output instead of
+    // 1.7e-3, and which of the two a row gets must not hang on the others of its batch.  The second product costs nothing where keys and values are
+    // waited for, 6 % where 128 queries share a prefix (64 rows 36.6 / 39.0 us), 27 % where the matrix cores are all there is (8 x 2048 tokens
+    // 2.33 / 2.95 ms).
+    __device__ __forceinline__ void values(const TileLane<T> &tl, const f32x16 &w, const u32x4 *vt) {
         if constexpr (sizeof(T) == 2) {
             const __attribute__((address_space(3))) char *base = (const __attribute__((address_space(3))) char *)(lptr_t)vt;
 #pragma unroll
@@ -311,14 +313,11 @@ template <typename T> struct Queries {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = w[8 * s + e];
                 const typename Elem<T>::Raw p = Elem<T>::from_float(x);
-                u32x4 rest;
-                if (REST) {
-                    float y[8];
-                    Elem<T>::to_float(p, y);
+                float y[8];
+                Elem<T>::to_float(p, y);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] -= y[e];
-                    rest = __builtin_bit_cast(u32x4, Elem<T>::from_float(x));
-                }
+                for (int e = 0; e < 8; ++e) x[e] -= y[e];
+                const u32x4 rest = __builtin_bit_cast(u32x4, Elem<T>::from_float(x));
 #pragma unroll
                 for (int d = 0; d < 4; ++d) {
                     typedef __attribute__((address_space(3))) s16x4 *tr_t;
@@ -326,7 +325,7 @@ template <typename T> struct Queries {
                     const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_t)(base + tl.vaddr[4 + d] + (16 * s + 8) * KeyTile<T>::ROWB)));
                     const u32x4 v = {lo[0], lo[1], hi[0], hi[1]};
                     M::mma(o[d], v, __builtin_bit_cast(u32x4, p));
-                    if (REST) M::mma(o[d], v, rest);
+                    M::mma(o[d], v, rest);
                 }
             }
         } else {

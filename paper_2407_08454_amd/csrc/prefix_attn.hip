@@ -191,7 +191,7 @@ __device__ __forceinline__ void split_unit(const PrefixAttnArgs &a, int u, u32x4
             qs.mask(x, there, tail ? qs.sees - j : 32);
         }
         qs.weights(x, a.c);
-        qs.template values<true>(tl, x, vt);
+        qs.values(tl, x, vt);
         wait_lds();
         if (j + 32 < end) load(V, vt);
     }
@@ -213,9 +213,10 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
 // The same for many queries: a workgroup of four waves has 128 of them and takes 64 keys at a time, which its waves load together and share.
 // What bounds it: matrix cores (38 % busy), vector ALU (39 %, the exponentials) and the fragments' way out of LDS beside one another: two
 // workgroups a compute unit, two waves a SIMD, so one wave's exponentials meet the other's products by chance.  8 x 2048 tokens of 40 heads over
-// 5734 states and their own: 2.1 ms, 900 TFLOP/s, where a library product of 8192^3 reaches 1130.  Tried and slower: eight waves that change
-// over between products and exponentials at barriers (2.35 ms: their LDS reads fall together), 64 queries a wave with a SIMD to itself (2.88),
-// fragments read ahead (2.21), one half's exponentials written between the other's products (2.30).
+// 5734 states and their own: 2.8 ms, 670 TFLOP/s (1010 with the weights' second product), where a library product of 8192^3 reaches 1130.  Tried
+// and slower, all without the second product, 2.1 ms: eight waves that change over between products and exponentials at barriers (2.35 ms:
+// their LDS reads fall together), 64 queries a wave with a SIMD to itself (2.88), fragments read ahead (2.21), one half's exponentials written
+// between the other's products (2.30).
 //   ROWS: the queries of one row and all their keys, prefix and tail one after the other in tiles of 64, in one part or several;
 //   else: the queries of a prompt's rows and a part of their prefix; the last workgroups have tail parts as above, one a wave.
 constexpr int PX_WIDE = 128;
@@ -368,8 +369,8 @@ __global__ __launch_bounds__(4 * WAVE, 2) void prefix_attn_wide_kernel(PrefixAtt
                 if (mixed && a.T > 1 && (has_nonfinite<T>(vt) || has_nonfinite<T>(vt + KT::SLOTS))) { stop = j; return; }
             }
             qs.weights(x0, x1, a.c);
-            qs.template values<false>(tl, x0, vt);
-            qs.template values<false>(tl, x1, vt + KT::SLOTS);
+            qs.values(tl, x0, vt);
+            qs.values(tl, x1, vt + KT::SLOTS);
         };
         uint64_t there_a = load(v, k_a, v_a), there_b = 0;
         for (;;) {

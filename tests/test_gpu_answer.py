@@ -443,6 +443,29 @@ def test_many_small_weights_beside_a_great_one(dtype, T, rows):
     _check(a.lse[:few], lse, l_tol, "lse")
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T,rows,H,G", [(1, 3, 2, 2), (5, 4, 2, 1), (1, 130, 1, 2), (150, 2, 2, 1), (130, 65, 4, 1)])
+def test_what_the_rounding_of_a_weight_leaves_is_not_lost(dtype, T, rows, H, G):
+    """Few queries, many rows of a prompt, many tokens of a row in parts and straight to the output: in every kernel the weights count with twice
+    the bits of their type, so that beside the output's own rounding there is a quarter of a step's square of a weight; small scores
+    keep what fp32 sums leave below that.  Weights with one rounding would be outside, as the plain form shows."""
+    _say(f"two-part weights {dtype} T={T} rows={rows} G={G}")
+    a = Attn(dtype, rows, T, H, G, 19, P=1, cap=12, kv=[T + 5] * rows, q_scale=0.25).run()
+    few, half = 2, ar.EPS[dtype] / 2
+    own = dict(a.pages64, table=a.pages64["table"][:few], kv_lens=a.pages64["kv_lens"][:few])
+    out, lse, (spread, worst, small) = ar.attention(a.q64[:few], G, None, a.prefix64, own)
+    tol = (half * half + 2 * worst)[..., None] * spread + (ar.TINY[dtype] / 2 * 2.0 ** -10 * small if dtype == "f16" else 0.0)
+    tol = tol * (1 + ar.EPS[dtype]) + half * np.abs(out) + ar.TINY[dtype]
+    _check(a.out[:few], out, tol, "out")
+    # the first token of row 0, head 0, with weights of one rounding
+    K, V = (np.concatenate([a.prefix64[x][0, 0], a.pages64[x][a.pages64["table"][0, 0], 0, :6]]) for x in ("K", "V"))
+    w = np.exp(K @ a.q64[0, 0, 0] / math.sqrt(128))
+    w /= w.max()
+    assert np.allclose(w @ V / w.sum(), out[0, 0, 0], rtol=0, atol=1e-12)
+    once = _stored(_stored(w, dtype)[0] @ V / w.sum(), dtype)[0]
+    assert (np.abs(once - out[0, 0, 0]) > tol[0, 0, 0]).any()
+
+
 def test_steps_without_tokens_and_batches_without_rows():
     tdt = torch.float16
     pool = [torch.full((3, 2, 4, 128), MARK, dtype=tdt, device="cuda") for _ in range(2)]
