@@ -427,8 +427,8 @@ typedef struct {
  * Appends a step's tokens to the paged cache, rotated to their positions on the way.  Token t of row b,
  * t < seq_lens[b], goes to slot s = past_lens[b] + t of the row and has position x = pos_base[b] + s; with
  * a = x * inv_freq[i] every pair (u, v) of a query or key head becomes (u cos a - v sin a, v cos a + u sin a);
- * values, and dimensions from rot_dim on, are stored as they are.  Angles are reduced in 64 bits, pairs turned
- * in fp32, one rounding to dtype.
+ * values, and dimensions from rot_dim on, are stored as they are.  Angles are reduced in 64 bits (fp32 caches: their
+ * sines and cosines are taken there too), pairs turned in fp32, one rounding to dtype.
  *   q_new     in   (B, T, H_kv*G, d), or NULL with q_out: keys and values alone
  *   k_new, v_new  in  (B, T, H_kv, d)
  *   past_lens in   [B] tokens in the row's pages before the call (clamped to [0, max_pages*page_size])

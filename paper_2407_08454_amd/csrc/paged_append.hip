@@ -27,13 +27,20 @@ struct AppendArgs {
 };
 
 // cos and sin of x f, x an integer: in 64 bits down to a fraction of a turn, so that far positions keep their angle (x f in fp32 is off
-// by 0.06 at x = 10^6), and from there in fp32.
-__device__ __forceinline__ float2 unit_at(int64_t x, float f) {
+// by 0.06 at x = 10^6).  From there fp32 caches go on in 64 bits, one rounding in the end: 2^-25 is all that a sine is off; with the fraction in
+// fp32 it was 2^-23 (6 x 301 tokens 14.5 us either way).  16-bit types round 2^13 times as coarsely: the rest in fp32.
+template <typename T> __device__ __forceinline__ float2 unit_at(int64_t x, float f) {
     double turns = (double)x * (double)f * 0.15915494309189533577;
     turns -= rint(turns);
-    float s, c;
-    sincospif((float)(2.0 * turns), &s, &c);
-    return make_float2(c, s);
+    if constexpr (sizeof(T) == 4) {
+        double s, c;
+        sincospi(2.0 * turns, &s, &c);
+        return make_float2((float)c, (float)s);
+    } else {
+        float s, c;
+        sincospif((float)(2.0 * turns), &s, &c);
+        return make_float2(c, s);
+    }
 }
 
 template <typename T, int STEPS, bool INTERLEAVED, bool STREAM>
@@ -76,7 +83,7 @@ __global__ __launch_bounds__(PA_BLOCK) void paged_append_kernel(AppendArgs a)
     int page = -1;
     if (slot < cap) page = a.table[(int64_t)b * a.max_pages + (slot >> a.page_shift)];
     const int64_t x = slot + (a.pos_base ? a.pos_base[b] : 0);
-    if (lane < a.rot / 2) units[wave][lane] = unit_at(x, a.inv_freq[lane]);
+    if (lane < a.rot / 2) units[wave][lane] = unit_at<T>(x, a.inv_freq[lane]);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");    // (a wave's LDS operations stay in order: it holds the compiler)
     __builtin_amdgcn_wave_barrier();
     float2 w[8];

@@ -112,6 +112,29 @@ def test_append_sizes(dtype, B, T, H, G, page, new, past, pos, fused):
     _append_case(dtype, B, T, H, G, page, 128, False, new, past, pos, 2, fused)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("pos", [0, 1000000])
+def test_append_angles_are_rounded_once(pos, interleaved):
+    """fp32: pairs (1, 0) become cosine and sine, each off by half a step at one, 2^-25, and by what the angle x f loses in 64 bits (two
+    roundings in the kernel, one and the functions' own in numpy)."""
+    T, H = 1500, 1
+    freq = (1.0 / 10000.0 ** (np.arange(0, 128, 2) / 128)).astype(np.float32)
+    x = torch.zeros((1, T, 3, 128), device="cuda")
+    x[..., 0::2] = 1.0
+    if not interleaved:
+        x[..., :64], x[..., 64:] = 1.0, 0.0
+    pool = [torch.zeros((-(-T // 64), H, 64, 128), device="cuda") for _ in range(2)]
+    pages = kb.make_pages(*pool, torch.arange(len(pool[0]), dtype=torch.int32, device="cuda")[None])
+    q_out, kv = torch.empty((1, T, 1, 128), device="cuda"), _i32([0])
+    kb.kvm_paged_append(kb.make_token_shape(pages, T, 1), pages, kb.make_rotation(torch.from_numpy(freq).cuda(), interleaved), x[:, :, :1],
+                        x[:, :, 1:2], x[:, :, 2:], _i32([0]), _i32([pos]), q_out, kv)
+    angle = (pos + np.arange(T, dtype=np.float64))[:, None] * freq.astype(np.float64)
+    want = np.stack([np.cos(angle), np.sin(angle)], 2 if interleaved else 1).reshape(T, 128)
+    tol = np.stack([2.0 ** -25 + 2.0 ** -50 * (1 + np.abs(angle))] * 2, 2 if interleaved else 1).reshape(T, 128)
+    _check(q_out[0, :, 0], want, tol, "queries")
+    _check(pool[0][:, 0].reshape(-1, 128)[:T], want, tol, "keys")
+
+
 @pytest.mark.parametrize("dtype,B,T", [("f16", 3, 7000), ("f32", 2, 5500)])
 def test_append_of_more_than_the_last_level_cache(dtype, B, T):
     """Large steps take the streaming kernel: rows of both ends against the plain form, and every value row against its source."""
