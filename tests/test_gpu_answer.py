@@ -544,6 +544,54 @@ def test_attention_repeats_its_bits_and_needs_no_lse(name, dtype):
     assert torch.equal(out, a.out)
 
 
+def _check_rows(a, rows):
+    """Rows of a call that is too large for the plain form as a whole."""
+    B, P = a.B, a.prefix64["K"].shape[0]
+    for b in rows:
+        p = ar.prompt_of(b, B, P, a.prefix64["row_start"])
+        pre = None if p < 0 else dict(K=a.prefix64["K"][p:p + 1], V=a.prefix64["V"][p:p + 1], lens=a.prefix64["lens"][p:p + 1], row_start=None)
+        own = dict(a.pages64, table=a.pages64["table"][b:b + 1], kv_lens=a.pages64["kv_lens"][b:b + 1])
+        out, lse, bounds = ar.attention(a.q64[b:b + 1], a.G, None if a.new is None else a.new[b:b + 1], pre, own)
+        o_tol, l_tol = ar.tolerance(a.dtype, out, lse, bounds)
+        there = ~np.isnan(lse)
+        out[~there], lse[~there], o_tol[~there], l_tol[~there] = MARK, MARK, 0.0, 0.0
+        _check(a.lse[b:b + 1], lse, l_tol, f"lse of row {b}")
+        _check(a.out[b:b + 1], out, o_tol, f"out of row {b}")
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_attention_over_more_than_the_last_level_cache(dtype, page):
+    """Lists so long that as many as there are of them fill half the last-level cache are read with the non-temporal hint: one such tail and two such prefixes,
+    of an odd number of keys, beside short ones, which are read without."""
+    _say(f"streaming {dtype} page={page}")
+    B, H, esz = 8, 32, 4 if dtype == "f32" else 2
+    long = (128 << 20) // (B * H * 2 * 128 * esz)              # keys a list from which on it is streamed
+    lens = [[long + 37] * H, [5] * H] + [[long // 2 + p] * H for p in range(2, B)]
+    lens[4] = [long + 1 if h % 2 else 0 for h in range(H)]
+    kv = [40, long + 75, 2, 3, 17, 64, 1, 33]
+    a = Attn(dtype, B, 2, H, 2, 20, P=B, cap=long + 37, lens=lens, kv=kv, page=page, new=[2, 2, 2, 1, 2, 0, 1, 2])
+    assert gu.kernels_of(a.call) == {"prefix_attn_split_kernel", "prefix_attn_join_kernel"}
+    a.run()
+    _check_rows(a, range(B))
+
+
+@pytest.mark.parametrize("dtype,T,G,kernel", [("f16", 1, 1, "prefix_attn_split_kernel"), ("f32", 2, 1, "prefix_attn_split_kernel"),
+                                              ("bf16", 2, 40, "prefix_attn_wide_kernel"), ("f32", 2, 40, "prefix_attn_split_kernel")])
+def test_more_prompts_than_a_wave_looks_through_at_once(dtype, T, G, kernel):
+    """150 prompts with none to 45 rows each, rows of no prompt at both ends."""
+    _say(f"many ragged prompts {dtype} T={T} G={G}")
+    counts = [(7 * p) % 4 for p in range(150)]
+    counts[3], counts[31], counts[32], counts[63], counts[64], counts[65], counts[100], counts[149] = 33, 0, 2, 1, 0, 45, 0, 3
+    starts = (2 + np.cumsum([0] + counts)).tolist()
+    B = starts[-1] + 2
+    a = Attn(dtype, B, T, 1, G, 21, P=150, cap=41, lens=[[(11 * p) % 42] for p in range(150)], row_start=starts, kv=[T + (5 * b) % 23 for b in range(B)], page=8)
+    assert kernel in gu.kernels_of(a.call)
+    a.run()
+    picked = range(B) if G == 1 else sorted({0, 1, 2, B - 1, B - 2, B - 3} | {starts[p] for p in range(0, 150, 9)} | {starts[65] + i for i in range(0, 45, 4)})
+    _check_rows(a, picked)
+
+
 def test_attention_beyond_32_bits():
     """Pools and prefixes of more than 2^32 elements: the last pages, the last prompt."""
     H, page, P, cap = 32, 64, 3, 400000
