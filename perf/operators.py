@@ -150,7 +150,8 @@ def prepare(case, seed):
     s.kind, s.H, s.G, s.rot, s.interleaved, s.page = kind, H, G, case["rot"], bool(case["interleaved"]), page
     new, tail = new_lengths(case), tail_lengths(case)
     s.new_lens = torch.tensor(new, **i32)
-    s.kv_lens = torch.tensor(tail, **i32)
+    # where the append writes the lengths, nothing that looks like them stands before the call
+    s.kv_lens = torch.tensor(tail, **i32) if kind == "attn" else torch.full((B,), -1, **i32)
     s.past_lens = torch.tensor([t - n for t, n in zip(tail, new)], **i32)
     # the tails: pages scattered over a pool, entries behind a row's last page are not in use
     used = [-(-t // page) for t in tail]
