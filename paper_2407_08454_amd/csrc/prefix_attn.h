@@ -437,10 +437,10 @@ __device__ __forceinline__ bool sums_broken(const Queries<T> &qs) {
 }
 
 // Does the value tile hold an infinity or a NaN?  Where some queries of a tile see a key that others do not (later tokens of the same
-// step), a weight of zero would not keep it out of the others' sums.
+// step), a weight of zero would not keep it out of the others' sums.  (16-bit types: the wide kernel's.)
 template <typename T>
 __device__ __forceinline__ bool has_nonfinite(const u32x4 *vt) {
-    constexpr uint32_t E = sizeof(T) == 4 ? 0x7F800000u : Elem<T>::kDtype == KVM_F16 ? 0x7C00u : 0x7F80u;
+    constexpr uint32_t E = Elem<T>::kDtype == KVM_F16 ? 0x7C00u : 0x7F80u;
     const int lane = threadIdx.x & 63;
     bool bad = false;
 #pragma unroll
@@ -449,8 +449,7 @@ __device__ __forceinline__ bool has_nonfinite(const u32x4 *vt) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const uint32_t x = v[k];
-            bad |= (x & E) == E;
-            if (sizeof(T) == 2) bad |= ((x >> 16) & E) == E;
+            bad |= (x & E) == E || ((x >> 16) & E) == E;
         }
     }
     return __ballot(bad) != 0;
