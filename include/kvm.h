@@ -436,7 +436,7 @@ typedef struct {
  *   q_out     out  (B, T, H_kv*G, d), contiguous; q_new itself if that is contiguous.  Tokens that are not
  *                  there (t >= seq_lens[b]) are left as they were
  *   kv_lens   out  [B] past + new, not beyond max_pages*page_size: what kvm_prefix_attn reads, and past_lens of
- *                  the next call.  A buffer of its own, not past_lens.
+ *                  the next call.  A buffer of its own: not past_lens, seq_lens or pos_base.
  * A token whose page the row does not have (see kvm_pages) or whose slot lies behind the table is not stored.
  * (A row that outgrows its table has to end: kv_lens stops at the table's end, and kvm_prefix_attn counts the step's tokens back
  * from there.)

@@ -482,6 +482,10 @@ kvm_status kvm_paged_append(const kvm_shape *shape, const kvm_pages *pages, cons
         set_error("%s: past_lens and kv_lens must be two buffers", fn);
         return KVM_ERR_INVALID_ARG;
     }
+    if (kv_lens == shape->seq_lens || kv_lens == pos_base) {    // read by some workgroups while another writes kv_lens
+        set_error("%s: kv_lens must be a buffer of its own, not seq_lens or pos_base", fn);
+        return KVM_ERR_INVALID_ARG;
+    }
     if (shape->N > 0) {
         if (rotation->rot_dim > 0 && !rotation->inv_freq) { set_error("%s: inv_freq must not be NULL", fn); return KVM_ERR_INVALID_ARG; }
         if (!q_new != !q_out) { set_error("%s: q_new and q_out go together", fn); return KVM_ERR_INVALID_ARG; }

@@ -84,6 +84,12 @@ def test_append_refuses(kw, code, word):
     assert _append(**kw) == code and word in _message()
 
 
+@pytest.mark.parametrize("kw", [dict(shape=_shape(seq_lens=8192)), dict(pos=TWO)])
+def test_append_refuses_lengths_that_are_written_over_what_it_reads(kw):
+    """kv_lens is written by one workgroup while others still read seq_lens and pos_base."""
+    assert _append(**kw) == kb.KVM_ERR_INVALID_ARG and "of its own" in _message()
+
+
 @pytest.mark.parametrize("kw,code,word", [
     (dict(shape=_shape(d=256)), kb.KVM_ERR_UNSUPPORTED, "head dimension"),
     (dict(shape=_shape(B=4096, N=4096)), kb.KVM_ERR_UNSUPPORTED, "too many"),
