@@ -148,8 +148,9 @@ static kvm_status launch_t(AppendArgs &a, bool interleaved, hipStream_t st)
         hipLaunchKernelGGL(kernel, dim3((unsigned)(a.token_blocks + (a.B + PA_BLOCK - 1) / PA_BLOCK)), dim3(PA_BLOCK), 0, st, a);
     };
     // Steps that the last-level cache cannot hold carry the non-temporal hint, and a wave has eight rows instead of sixteen.  us, plain with 16 rows /
-    // hint with 16 / hint with 8: 16384 tokens of 40 heads in fp16 (1.0 GB) 190 / 181 / 172, 8192 in fp32 194 / 202 / 179; smaller ones
-    // differ by less than their runs do.
+    // hint with 16 / hint with 8: 16384 tokens of 40 heads in fp16 (1.0 GB) 190 / 181 / 172, 8192 in fp32 194 / 202 / 179.  Plain with 8 rows, beside the
+    // present choice: these two 176 / 169 and 179 / 181, 403 MB of fp16 74 / 70, 101 MB 17.9 / 17.3, 59 MB of fp32 13.6 / 13.7; where the
+    // bytes are just the cache's (268 MB, and the same buffers every time) 42 / 51.
     if ((int64_t)a.B * a.T * rows * HEAD_DIM * (int)sizeof(T) * 2 >= LLC_BYTES)
         interleaved ? run(paged_append_kernel<T, 1, true, true>, 1) : run(paged_append_kernel<T, 1, false, true>, 1);
     else

@@ -98,8 +98,8 @@ __device__ __forceinline__ int parts_of_prefix(const PrefixAttnArgs &a, int n) {
 
 // What bounds it: the read of the keys and values (fp32: the matrix cores, 8192 cycles a tile of 32 keys).  A wave has room for one tile of 32
 // keys and one of their values in LDS: the next keys are asked for as soon as the scores are taken, the next values when they have been added
-// up, so that one of the two is always on its way and mostly both; eight waves of a compute unit keep 128 KB on their way (two stages a wave,
-// four waves: 37 rows over 2048 states and tails of up to 1000 tokens 88 us, this 72).  Nobody waits for anybody.  8 rows with tails of up to
+// up, so that one of the two is always on its way and mostly both; eight waves of a compute unit (fp32: four, of tiles twice as large) keep 128 KB
+// on their way (two stages a wave, four waves: 37 rows over 2048 states and tails of up to 1000 tokens 88 us, this 72).  Nobody waits for anybody.  8 rows with tails of up to
 // 16384 tokens, 1.76 GB: 284 us, 6.2 TB/s.
 //   u: tail parts first (their keys are found by way of lengths and page table, and they may be the longer ones), then prefix parts.
 template <typename T>
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
 }
 
 // The same for many queries: a workgroup of four waves has 128 of them and takes 64 keys at a time, which its waves load together and share.
-// What bounds it: matrix cores (38 % busy), vector ALU (39 %, the exponentials) and the fragments' way out of LDS beside one another: two
+// What bounds it: matrix cores (50 % busy), vector ALU (49 %, their issue among it) and the fragments' way out of LDS beside one another: two
 // workgroups a compute unit, two waves a SIMD, so one wave's exponentials meet the other's products by chance.  8 x 2048 tokens of 40 heads over
 // 5734 states and their own: 2.8 ms, 670 TFLOP/s (1010 with the weights' second product), where a library product of 8192^3 reaches 1130.  Tried
 // and slower, all without the second product, 2.1 ms: eight waves that change over between products and exponentials at barriers (2.35 ms:
@@ -568,7 +568,9 @@ static void plan(const kvm_shape &sh, const kvm_prefix *prefix, const kvm_pages 
             a.splits_p = (int)std::max<int64_t>(1, std::min<int64_t>(256 / wide_prompts, a.cap / 256));
         }
     }
-    // A compute unit holds eight waves of the split kernel.  The tails get parts for all of them, the prefixes for what the tails leave, a
+    // A compute unit holds eight waves of the split kernel (fp32: four, by their registers and LDS, but it takes parts for eight all the same: half
+    // as many, us, 16 rows of 4 tokens over 4000 states 87 instead of 48, 8 rows with tails of up to 2000 tokens 185 instead of 138, 4 rows with 8000
+    // 71 instead of 77, one row 31 instead of 36).  The tails get parts for all of them, the prefixes for what the tails leave, a
     // quarter at least: their parts are joined for every one of their rows.  (32 rows of two prompts, us, both launches, prefixes and tails in 16
     // and 1 / 8 and 1 / 8 and 2 / 4 and 2 parts 57 / 52 / 44 / 47.)
     int64_t units_t = 0;
@@ -627,7 +629,8 @@ static kvm_status launch_t(const PrefixAttnArgs &a, hipStream_t st)
     const int parts = a.splits_p + a.splits_t;
     if (parts <= JOIN_AHEAD) join(prefix_attn_join_kernel<T, 1>, 1);
     else if (parts <= 2 * JOIN_AHEAD) join(prefix_attn_join_kernel<T, 2>, 2);
-    // (eight groups where rows are few; 2048 rows of 20 parts, us, by eight / four / two groups 9.0 / 7.9 / 8.7, 32 of 34 5.5 / 7.2 / 10.1)
+    // (eight groups where rows are few, us by eight / four: 256 rows of 130 parts 12.8 / 20.7, 768 of 44 9.6 / 11.2, 1024 of 34 10.0 / 10.2, 1024 of 18
+    // 8.4 / 8.2, 1280 of 18 9.3 / 8.7, 2048 of 20 11.3 / 10.6; by two groups 2048 rows take longer again)
     else if (parts <= 4 * JOIN_AHEAD || query_rows(a) > 1024) join(prefix_attn_join_kernel<T, 4>, 4);
     else join(prefix_attn_join_kernel<T, 8>, 8);
     return check_launch("prefix_attn_join_kernel");
