@@ -392,6 +392,12 @@ static __device__ __attribute__((noinline)) void one_by_one(LaneState *st, KeySo
     st->m = m;
     st->l = l;
 }
+// tokens of row b or states of prefix (p, h)
+template <typename T> __device__ __forceinline__ KeySource key_source(const PrefixAttnArgs &a, bool tail, int p, int b, int h) {
+    const size_t at = ((size_t)max(p, 0) * a.H + h) * a.cap * HEAD_DIM;
+    return {tail ? a.Kt : (const T *)a.Kp + at, tail ? a.Vt : (const T *)a.Vp + at, tail ? a.table + (size_t)b * a.max_pages : nullptr, a.n_pages,
+            a.page_shift, a.H, h, a.c};
+}
 // states [first_p, last_p) of prefix (p, h) and tokens [first_t, last_t) of row b for a wave's queries; afresh: instead of what they have
 template <typename T>
 __device__ __forceinline__ void one_by_one(const PrefixAttnArgs &a, Queries<T> &qs, int p, int b, int h, int first_p, int last_p, int first_t, int last_t,
@@ -405,14 +411,11 @@ __device__ __forceinline__ void one_by_one(const PrefixAttnArgs &a, Queries<T> &
     st.l = afresh ? 0.f : qs.l;
     const int64_t HG = a.H * a.G, token = qs.valid ? qs.row / HG : 0, head = qs.valid ? qs.row - token * HG : 0;
     const T *q = (const T *)a.q + token * a.q_stride + head * HEAD_DIM;
-    const size_t at = ((size_t)max(p, 0) * a.H + h) * a.cap * HEAD_DIM;
 #pragma unroll 1
     for (int tail = 0; tail < 2; ++tail) {                    // (a loop, so that the call stands here once)
         const int first = tail ? first_t : first_p, last = tail ? last_t : last_p;
         if (first >= last) continue;
-        const KeySource src = {tail ? a.Kt : (const T *)a.Kp + at, tail ? a.Vt : (const T *)a.Vp + at,
-                               tail ? a.table + (size_t)b * a.max_pages : nullptr, a.n_pages, a.page_shift, a.H, h, a.c};
-        one_by_one<T>(&st, src, q, !qs.valid ? 0 : tail ? qs.sees : last, first, last);
+        one_by_one<T>(&st, key_source<T>(a, tail, p, b, h), q, !qs.valid ? 0 : tail ? qs.sees : last, first, last);
     }
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -434,6 +437,33 @@ __device__ __forceinline__ bool sums_broken(const Queries<T> &qs) {
         for (int i = 0; i < 16; ++i) finite = fmaf(qs.o[d][i], 0.f, finite);
     const float l = qs.l + other_half(qs.l);
     return __ballot(qs.valid && finite != 0.f && l - l == 0.f) != 0;
+}
+
+// The infinities and NaN among values [first, last) of a list, added up: dimensions 2 lane and 2 lane + 1 (16-bit types).  A query that sees all of
+// these keys has just that in such a dimension, whatever the weights.  One read of the values, where taking the keys one by one is a round trip each.
+template <typename T>
+static __device__ __forceinline__ void add_nonfinite(float sum[2], const KeySource &src, int first, int last) {
+    for (int j = first, end; j < last; j = end) {
+        size_t at = j;
+        end = last;
+        if (src.table) {
+            const int page = src.table[j >> src.page_shift], mask = (1 << src.page_shift) - 1;
+            end = min(last, (j | mask) + 1);
+            if (page < 0 || page >= src.n_pages) continue;
+            at = (((size_t)page * src.H + src.h) << src.page_shift) + (j & mask);
+        }
+        const T *row = (const T *)src.V + at * HEAD_DIM + 2 * (threadIdx.x & 63);
+#pragma unroll 8
+        for (int i = j; i < end; ++i, row += HEAD_DIM) {
+            T v[2];
+            __builtin_memcpy(v, row, sizeof(v));
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float x = (float)v[e];
+                sum[e] += x - x == 0.f ? 0.f : x;
+            }
+        }
+    }
 }
 
 // Does the value tile hold an infinity or a NaN?  Where some queries of a tile see a key that others do not (later tokens of the same

@@ -388,10 +388,27 @@ __global__ __launch_bounds__(4 * WAVE, 2) void prefix_attn_wide_kernel(PrefixAtt
             if (++v >= v_end) break;
         }
     }
-    const bool again = sums_broken(qs);                      // all of the part once more
+    // Sums that are not finite: of values that are not, which all of the wave's queries see (a tile that only some see has none), so
+    // that each stands for itself in its dimension, or of finite ones beyond fp32: then all of the part once more.
+    bool again = false;
+    if (sums_broken(qs)) {
+        const int first_p = 64 * part * per_part, last_p = min(n, 64 * v_end), first_t = 64 * max(part * per_part - tiles_n, 0);
+        float sum[2] = {0.f, 0.f};
+        add_nonfinite<T>(sum, key_source<T>(a, false, p, b, h), first_p, last_p);
+        if (ROWS) add_nonfinite<T>(sum, key_source<T>(a, true, p, b, h), first_t, min(stop, tail_end));
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {                   // dimension 32 d + acc_row(i)
+                const float own = qs.o[d][i], of_values = __shfl(sum[i & 1], 16 * d + 4 * (i >> 2) + 2 * (lane >> 5) + ((i & 3) >> 1), WAVE);
+                if (of_values != 0.f) qs.o[d][i] = of_values;
+                else again |= qs.valid && own - own != 0.f;
+            }
+        again = __ballot(again) != 0;
+    }
     if (again || (ROWS && !idle && stop < tail_end)) {
-        const int v_first = part * per_part, first_t = again ? 64 * max(v_first - tiles_n, 0) : stop;
-        one_by_one<T>(a, qs, p, b, h, 64 * v_first, again ? min(n, 64 * v_end) : 0, first_t, ROWS ? tail_end : 0, again);
+        const int first_t = again ? 64 * max(part * per_part - tiles_n, 0) : stop;
+        one_by_one<T>(a, qs, p, b, h, 64 * part * per_part, again ? min(n, 64 * v_end) : 0, first_t, ROWS ? tail_end : 0, again);
     }
     const float l = qs.l + other_half(qs.l);
     if (!qs.valid) return;

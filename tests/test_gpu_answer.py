@@ -443,6 +443,59 @@ def test_an_infinite_value_under_a_small_weight_stays_infinite(dtype, T, rows, H
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,rows,H", [(1, 3, 2), (1, 200, 2), (150, 2, 2), (130, 65, 4)])
+@pytest.mark.parametrize("page", [2, 64])
+def test_a_nan_that_is_seen_stays_in_its_dimension(dtype, T, rows, H, page):
+    """Also what two infinities of different signs make; beside them an infinity that is seen, and a NaN that only the last token sees."""
+    _say(f"seen NaN {dtype} T={T} rows={rows} page={page}")
+    a = Attn(dtype, rows, T, H, 1, 22, P=1, cap=150, kv=[T + 190] * rows, page=page)
+    put = lambda x64, x, at, value: (x64.__setitem__(at, value), x.__setitem__(at, value))
+    (_, pre_v, _, _), (_, own_v, _) = a.prefix._refs, a.pages._refs
+    own = lambda b, j, d: np.s_[a.pages64["table"][b, j // page], 1, j % page, d]
+    put(a.prefix64["V"], pre_v, np.s_[0, 0, 133, 7], np.nan)
+    put(a.prefix64["V"], pre_v, np.s_[0, 0, 2, 8], np.inf)
+    put(a.prefix64["V"], pre_v, np.s_[0, 1, 3, 127], -np.inf)
+    put(a.pages64["V"], own_v, own(0, 71, 127), np.inf)        # meets the last one, in row 0 alone
+    put(a.pages64["V"], own_v, own(1, 5, 0), -np.inf)
+    put(a.pages64["V"], own_v, own(1, T + 189, 1), np.nan)     # the last token's own
+    a.run()
+    assert (a.out == MARK).sum() == 0
+    few = 2 if T > 1 else 3
+    with np.errstate(invalid="ignore"):                        # inf - inf is meant
+        want, lse, bounds = ar.attention(a.q64[:few], 1, None, a.prefix64, dict(a.pages64, table=a.pages64["table"][:few], kv_lens=a.pages64["kv_lens"][:few]))
+    o_tol, l_tol = ar.tolerance(dtype, want, lse, tuple(np.nan_to_num(x, nan=0.0, posinf=0.0) for x in bounds))
+    nans = np.zeros(want.shape, bool)
+    nans[:, :, 0, 7], nans[0, :, 1, 127], nans[1, T - 1, 1, 1] = True, True, True
+    assert (np.isnan(want) == nans).all() and np.isinf(want).sum() == few * T + (few - 1) * T + T
+    o_tol[~np.isfinite(want)] = 0.0
+    _check(a.out[:few], want, o_tol, "out")
+    _check(a.lse[:few], lse, l_tol, "lse")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,rows,H", [(1, 3, 1), (1, 200, 1), (150, 2, 1), (130, 65, 4)])
+def test_great_values_under_a_reference_that_lags(dtype, T, rows, H):
+    """A later state with a score five above the ones before it has a weight of 2^7 against their reference: with a value of 2^125 the sum is beyond
+    fp32, though the output is not."""
+    _say(f"great values {dtype} T={T} rows={rows}")
+    a = Attn(dtype, rows, T, H, 1, 23, P=1, cap=150)
+    a.prefix64["K"][...] = 0.0
+    a.prefix64["K"][:, :, 130, 0] = 4.0                        # 14.25 * 4 / sqrt(128) = 5.04
+    a.prefix64["V"][:, :, 130] = 2.0 ** 125 * (1 - 2 * (np.arange(128) % 2))
+    a.q64[...] = 0.0
+    a.q64[..., 0] = 14.25
+    for x64, x in ((a.prefix64["K"], a.prefix._refs[0]), (a.prefix64["V"], a.prefix._refs[1]), (a.q64, a.q)):
+        x.copy_(torch.from_numpy(x64))
+    a.run()
+    few = min(rows, 2)
+    out, lse, bounds = ar.attention(a.q64[:few], 1, None, a.prefix64, None)
+    o_tol, l_tol = ar.tolerance(dtype, out, lse, bounds)
+    _check(a.out[:few], out, o_tol, "out")
+    _check(a.lse[:few], lse, l_tol, "lse")
+    assert torch.isfinite(a.out).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("T,rows", [(1, 2), (1, 200), (150, 2)])
 def test_many_small_weights_beside_a_great_one(dtype, T, rows):
     """A first state with nearly all of the weight and a value of zero, as models have them: the output is what thousands of weights of
