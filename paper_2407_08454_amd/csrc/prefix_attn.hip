@@ -211,9 +211,9 @@ __global__ __launch_bounds__(WAVE, sizeof(T) == 2 ? 2 : 1) void prefix_attn_spli
 }
 
 // The same for many queries: a workgroup of four waves has 128 of them and takes 64 keys at a time, which its waves load together and share.
-// What bounds it: matrix cores (50 % busy), vector ALU (49 %, their issue among it) and the fragments' way out of LDS beside one another: two
+// What bounds it: matrix cores (49 % busy), vector ALU (48 %, their issue among it) and the fragments' way out of LDS beside one another: two
 // workgroups a compute unit, two waves a SIMD, so one wave's exponentials meet the other's products by chance.  8 x 2048 tokens of 40 heads over
-// 5734 states and their own: 2.8 ms, 670 TFLOP/s (1010 with the weights' second product), where a library product of 8192^3 reaches 1130.  Tried
+// 5734 states and their own: 2.8 ms, 680 TFLOP/s (1020 with the weights' second product), where a library product of 8192^3 reaches 1130.  Tried
 // and slower, all without the second product, 2.1 ms: eight waves that change over between products and exponentials at barriers (2.35 ms:
 // their LDS reads fall together), 64 queries a wave with a SIMD to itself (2.88), fragments read ahead (2.21), one half's exponentials written
 // between the other's products (2.30).
